@@ -306,6 +306,108 @@ dropit_status dropit_conv_weight_grad(const void* dy, const void* values, const 
                                       int accumulate, void* workspace, size_t workspace_bytes, int32_t* dev_status,
                                       void* cuda_stream);
 
+/*
+ * The first half of a gated feed-forward block: h = f(a) * u with a = x Wg^T + bg and u = x Wu^T + bu, one kernel for both
+ * products, the gate function and their product.  Its weight gradient, the layer's only use of x, comes from the cache of x as any
+ * Linear's does: dropit_weight_grad with dy = dgu [M x 2H] (Eq. 6).
+ *   w [device, 2H x C row-major, dtype]: the gate's H rows, then the other H; bias [device, 2H, dtype] or NULL; the same order holds for
+ *   gu and dgu [device, M x 2H row-major]: a | u and their gradients.
+ *   gate: f = SiLU x / (1 + e^-x), GELU x Phi(x), or ReLU.
+ *   dropit_gated_linear: x [device, M x C] -> h [device, M x H] and, unless NULL, gu (what the backward pass reads).  Sums in fp32, h from
+ *     the unrounded sums.
+ *   dropit_gated_linear_backward: dh [device, M x H], gu -> dgu = dh u f'(a) | dh f(a) and, unless NULL, db [device, 2H, dtype], the
+ *     column sums of the unrounded dgu (fp32, a fixed order); workspace of dropit_gated_linear_backward_workspace bytes (0 without db),
+ *     contents destroyed, need not be initialised.
+ *   dropit_gated_input_grad: dx [device, M x C] = dgu W (Eq. 3).
+ * bf16 with C and H multiples of 8 multiplies on the tensor cores; fp32 and other widths with fp32 FMA.  M = 0 is a no-op (db is zeroed); C, H >= 1;
+ * M * C, M * 2H and 2H * C < 2^31 each.
+ */
+typedef enum { DROPIT_GATE_SILU = 0, DROPIT_GATE_GELU = 1, DROPIT_GATE_RELU = 2 } dropit_gate;
+dropit_status dropit_gated_linear(const void* x, const void* w, const void* bias, int64_t M, int64_t C, int64_t H, dropit_dtype dtype,
+                                  dropit_gate gate, void* h, void* gu, int32_t* dev_status, void* cuda_stream);
+dropit_status dropit_gated_linear_backward_workspace(int64_t M, int64_t H, dropit_dtype dtype, size_t* workspace_bytes);
+dropit_status dropit_gated_linear_backward(const void* dh, const void* gu, int64_t M, int64_t H, dropit_dtype dtype, dropit_gate gate,
+                                           void* dgu, void* db, void* workspace, size_t workspace_bytes, void* cuda_stream);
+dropit_status dropit_gated_input_grad(const void* dgu, const void* w, int64_t M, int64_t C, int64_t H, dropit_dtype dtype, void* dx,
+                                      int32_t* dev_status, void* cuda_stream);
+
+/*
+ * Rotary positions with several axes (rows and columns of an image; time, height and width of a video).  Pair j of every head turns by
+ * the angle p[axis(j)] * theta^-e(j): (a, b) -> (a cos - b sin, a sin + b cos).
+ *   dropit_rotary_make_plan [host]: `sections` = channels per axis (even, their sum the rotated channels, the rest of a head stays as it is), in
+ *     the order in which the pairs are dealt out.  e(j) = 2i / sections[axis], i counted within the axis, or with `shared` 2j / rotated
+ *     (one ladder of frequencies dealt out to the axes).  interleaved: pair j = channels (2j, 2j + 1), else (j, j + rotated / 2).  theta >= 1;
+ *     up to DROPIT_ROTARY_MAX_PAIRS pairs and DROPIT_ROTARY_MAX_AXES axes.
+ *   dropit_rotary: queries and, unless NULL, keys, [batch, length, heads, head_dim] each with strides of its own in elements (the channels of a
+ *     head lie together; element-aligned is enough); out may be in with the same strides, any other overlap is not allowed.
+ *     positions [device], strides in elements (0 repeats).  Whole numbers (32 or 64 bits): the angle is exact to 2^-31 of a turn for |p| < 2^31.
+ *     fp32: the product is formed in 64-bit floats.  inverse: by the negative angle, which is the gradient.
+ */
+#define DROPIT_ROTARY_MAX_PAIRS 256
+#define DROPIT_ROTARY_MAX_AXES 8
+typedef enum { DROPIT_POSITION_I32 = 0, DROPIT_POSITION_I64 = 1, DROPIT_POSITION_F32 = 2 } dropit_position_type;
+typedef struct {
+    int32_t head_dim, pairs, axes, interleaved;
+    uint64_t turns[DROPIT_ROTARY_MAX_PAIRS];     /* turns per position, as a fraction of 2^64 */
+    uint8_t axis[DROPIT_ROTARY_MAX_PAIRS];
+} dropit_rotary_plan;
+typedef struct {
+    const void* in;
+    void* out;
+    int64_t in_batch, in_token, in_head, out_batch, out_token, out_head;
+    int32_t heads;
+} dropit_rotary_tensor;
+dropit_status dropit_rotary_make_plan(int head_dim, const int* sections, int axes, double theta, int shared, int interleaved,
+                                      dropit_rotary_plan* plan);
+dropit_status dropit_rotary(const dropit_rotary_plan* plan, int64_t batch, int64_t length, const dropit_rotary_tensor* q,
+                            const dropit_rotary_tensor* k, const void* positions, dropit_position_type position_type, int64_t pos_batch,
+                            int64_t pos_token, int64_t pos_axis, dropit_dtype dtype, int inverse, void* cuda_stream);
+
+/*
+ * One AdamW step over many tensors: m = b1 m + (1 - b1) g, v = b2 v + (1 - b2) g^2,
+ * p = (1 - lr wd) p - lr (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps), in fp32.
+ * The moments of all tensors lie in arenas: tensor i has ceil(n / DROPIT_ADAMW_BLOCK) blocks of DROPIT_ADAMW_BLOCK values from
+ * first_block on; what lies behind its n-th value is zero and stays zero.  Tensors of one call share no blocks, no ordinals and no memory.
+ *   state_bits 32: exp_avg, exp_avg_sq are fp32.  state_bits 8: both hold 8-bit floats (e4m3: sign, 4 exponent and 3 mantissa bits) of m and of
+ *     sqrt(v), value = code * scale, one fp32 scale per block = largest magnitude / 448 (0 below 1e-30; NaN if any is not finite).
+ *     A value between two codes takes the upper one if its place between them plus r / 65536 reaches one; sqrt(v) > 0 has code
+ *     2^-9 at least.  r: the high (m) and low (sqrt v) halves of mix(i ^ mix(mix(mix(seed) + t) + ordinal)), i the value's place in its tensor, t
+ *     the step's number, mix(x) = x ^= x >> 16; x *= 0x7FEB352D; x ^= x >> 15; x *= 0x846CA68B; x ^= x >> 16 (32 bits).
+ *   dither (bf16 parameters): p is rounded up to the next bf16 in the same way, r the high half of that word times 0x9E3779B1; else to nearest.
+ *   master (bf16 parameters) or NULL: the parameters in fp32, laid out as the moments; p is then written only.
+ *   steps [device, int32 per ordinal]: steps taken; the call counts up those of its tensors (not those with n = 0).  ticket [device, one word]: zero
+ *     before the first call, zero again after each; calls with the same ticket are ordered.  grad_factor [device] or NULL: multiplies the
+ *     gradients.  lr_device [device] or NULL: read in the place of lr.
+ * All tensors of a call have the same types; nothing is copied to the device, so that a captured call replays with its step number counting on.
+ */
+#define DROPIT_ADAMW_BLOCK 256
+typedef struct {
+    void* param;
+    const void* grad;
+    const float* lr_device;
+    int64_t n, first_block;
+    int32_t ordinal;
+    float lr, weight_decay;
+} dropit_adamw_tensor;
+typedef struct {
+    dropit_dtype param_dtype, grad_dtype;
+    int32_t state_bits, dither;
+    double beta1, beta2, eps;
+    uint32_t seed;
+} dropit_adamw_options;
+typedef struct {
+    void* exp_avg;
+    void* exp_avg_sq;
+    float* exp_avg_scale;
+    float* exp_avg_sq_scale;
+    float* master;
+    int32_t* steps;
+    uint32_t* ticket;
+    const float* grad_factor;
+} dropit_adamw_state;
+dropit_status dropit_adamw_step(const dropit_adamw_tensor* tensors, int count, const dropit_adamw_options* options,
+                                const dropit_adamw_state* state, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -12,7 +12,11 @@ from .api import (  # noqa: F401
     dropit_weight_grad_workspace, check_device_status, library_path,
     dropit_activation_table, dropit_produce, dropit_produce_workspace, dropit_compress_prepared,
     dropit_quantize_cache, dropit_dequantize_cache,
+    dropit_gated_linear, dropit_gated_linear_backward, dropit_gated_input_grad,
+    dropit_rotary, dropit_rotary_plan,
 )
 from .nn import (  # noqa: F401
-    DropITConv2d, DropITConv2dFn, DropITGeluLinear, DropITGeluLinearFn, DropITLinear, DropITLinearFn, convert_linear_layers,
+    DropITConv2d, DropITConv2dFn, DropITGatedLinear, DropITGeluLinear, DropITGeluLinearFn, DropITLinear, DropITLinearFn, DropITRotary,
+    convert_linear_layers,
 )
+from .optim import DropITAdamW  # noqa: F401

@@ -43,6 +43,13 @@ SIGNATURES = {
     "dropit_conv_weight_grad_workspace": (c_int, [c_int] * 9 + [c_int, c_int, p_sz]),
     "dropit_conv_weight_grad": (c_int, [c_vp, c_vp, c_vp, c_vp] + [c_int] * 10 + [c_i64, c_int, c_int, c_vp, c_int,
                                         c_vp, c_sz, c_vp, c_vp]),
+    "dropit_gated_linear": (c_int, [c_vp, c_vp, c_vp, c_i64, c_i64, c_i64, c_int, c_int, c_vp, c_vp, c_vp, c_vp]),
+    "dropit_gated_linear_backward_workspace": (c_int, [c_i64, c_i64, c_int, p_sz]),
+    "dropit_gated_linear_backward": (c_int, [c_vp, c_vp, c_i64, c_i64, c_int, c_int, c_vp, c_vp, c_vp, c_sz, c_vp]),
+    "dropit_gated_input_grad": (c_int, [c_vp, c_vp, c_i64, c_i64, c_i64, c_int, c_vp, c_vp, c_vp]),
+    "dropit_rotary_make_plan": (c_int, [c_int, ctypes.POINTER(c_int), c_int, c_dbl, c_int, c_int, c_vp]),
+    "dropit_rotary": (c_int, [c_vp, c_i64, c_i64, c_vp, c_vp, c_vp, c_int, c_i64, c_i64, c_i64, c_int, c_int, c_vp]),
+    "dropit_adamw_step": (c_int, [c_vp, c_int, c_vp, c_vp, c_vp]),
 }
 
 

@@ -343,3 +343,55 @@ def dropit_conv_weight_grad(dy: torch.Tensor, cache: DropITCache, kernel_size: T
     R, S = kernel_size
     return _native().conv_weight_grad(dy, cache.values, cache.meta, cache.offsets, B, Ca, H, W, R, S, stride, pad, dilation, cache.k,
                                       cache.fmt, out, accumulate, workspace)
+
+
+GATE_SILU, GATE_GELU, GATE_RELU = 0, 1, 2
+_GATE = {"silu": GATE_SILU, "gelu": GATE_GELU, "relu": GATE_RELU}
+
+
+def _gate_code(gate: str) -> int:
+    if gate not in _GATE:
+        raise ValueError("gate must be one of %s, got %r" % (", ".join(sorted(_GATE)), gate))
+    return _GATE[gate]
+
+
+def dropit_gated_linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, gate: str = "silu",
+                        keep: bool = False):
+    """h = f(a) * u with a | u = x W^T + b: the first half of a gated feed-forward block in one kernel.  weight [2 * hidden, channels]
+    and bias [2 * hidden]: the gate's half first.  f: "silu", "gelu" or "relu".  keep: returns (h, gu), gu = a | u for the backward pass.
+    bf16 or fp32, any leading dimensions; sums in fp32, one rounding.  No autograd: that is nn.DropITGatedLinear."""
+    h, gu = _native().gated_linear(x, weight, bias, _gate_code(gate), bool(keep))
+    return (h, gu) if keep else h
+
+
+def dropit_gated_linear_backward(dh: torch.Tensor, gu: torch.Tensor, gate: str = "silu", bias_grad: bool = False):
+    """dgu = dh u f'(a) | dh f(a) from what dropit_gated_linear kept; with bias_grad (dgu, db), db the column sums of the unrounded
+    dgu.  dW is dropit_weight_grad(dgu, cache of x), dx is dropit_gated_input_grad(dgu, weight)."""
+    dgu, db = _native().gated_linear_backward(dh, gu, _gate_code(gate), bool(bias_grad))
+    return (dgu, db) if bias_grad else dgu
+
+
+def dropit_gated_input_grad(dgu: torch.Tensor, weight: torch.Tensor) -> torch.Tensor:
+    """dx = dgu W (Eq. 3)."""
+    return _native().gated_input_grad(dgu, weight)
+
+
+def dropit_rotary_plan(head_dim: int, sections, theta: float = 10000.0, interleaved: bool = False, shared: bool = False) -> torch.Tensor:
+    """What dropit_rotary needs to know beside the positions: `sections` = channels per axis (even; their sum is rotated, the rest of a
+    head stays as it is); interleaved: pairs of neighbours, else of the two halves of the rotated channels; shared: one ladder of frequencies
+    theta^(-2j / rotated) dealt out to the axes, else a ladder theta^(-2i / section) for each axis.  A host object (a CPU tensor of bytes)."""
+    sections = [int(s) for s in sections]
+    if int(head_dim) < 2 or not sections or any(s < 0 or s % 2 for s in sections) or not 2 <= sum(sections) <= int(head_dim):
+        raise ValueError("sections must be even and sum up to 2 .. head_dim, got %r for %r" % (sections, head_dim))
+    if not float(theta) >= 1:
+        raise ValueError("theta must be at least 1, got %r" % (theta,))
+    return _native().rotary_plan(int(head_dim), sections, float(theta), bool(shared), bool(interleaved))
+
+
+def dropit_rotary(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor, plan: torch.Tensor, inverse: bool = False,
+                  in_place: bool = False):
+    """Queries and, unless None, keys turned by their positions: (q', k').  q [batch, length, heads, head_dim] or [length, heads, head_dim],
+    bf16 or fp32, any strides as long as the channels of a head lie together; k the same with heads of its own.  positions
+    [length, axes] or [batch, length, axes], int32, int64 or fp32.  Results are contiguous, or written over q and k with in_place.
+    No autograd: that is nn.DropITRotary."""
+    return _native().rotary(q, k, positions, plan, bool(inverse), bool(in_place))

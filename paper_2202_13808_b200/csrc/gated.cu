@@ -1,0 +1,306 @@
+// The gated linear (see include/dropit.h): entry points, the element-wise part of the backward pass, and the products in fp32 FMA.
+#include "gated.h"
+
+#include <algorithm>
+
+namespace dropit {
+
+namespace {
+
+__device__ __forceinline__ float to_float(uint16_t b) { return __uint_as_float((uint32_t)b << 16); }
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ void put(uint16_t* p, float v) { *p = (uint16_t)pack_bf16(v, 0.f); }
+__device__ __forceinline__ void put(float* p, float v) { *p = v; }
+
+// ---------------------------------------------------------------------------------------------
+// Products in fp32 FMA: fp32 tensors, and bf16 widths that the tensor-core kernels do not take.  64 x 64 outputs a CTA, 4 x 4 a thread
+// (two of them in the forward pass: the gate's and the other).
+// ---------------------------------------------------------------------------------------------
+constexpr int kTile = 64, kStep = 16, kFmaThreads = 256;
+
+// rows x kStep of a row-major matrix [rows_total x k_total] from (row0, k0), transposed into tile[k][row]
+template <typename T>
+__device__ __forceinline__ void stage_rows(float (&tile)[kStep][kTile + 4], const T* a, int64_t row0, int64_t rows_total, int64_t k0, int64_t k_total) {
+    for (int i = threadIdx.x; i < kTile * kStep; i += kFmaThreads) {
+        const int k = i % kStep, r = i / kStep;
+        tile[k][r] = row0 + r < rows_total && k0 + k < k_total ? to_float(a[(row0 + r) * k_total + k0 + k]) : 0.f;
+    }
+}
+// kStep x cols of a row-major matrix [k_total x cols_total]
+template <typename T>
+__device__ __forceinline__ void stage_cols(float (&tile)[kStep][kTile + 4], const T* b, int64_t k0, int64_t k_total, int64_t col0, int64_t cols_total) {
+    for (int i = threadIdx.x; i < kTile * kStep; i += kFmaThreads) {
+        const int c = i % kTile, k = i / kTile;
+        tile[k][c] = k0 + k < k_total && col0 + c < cols_total ? to_float(b[(k0 + k) * cols_total + col0 + c]) : 0.f;
+    }
+}
+__device__ __forceinline__ void multiply(float (&acc)[4][4], const float (&a)[kStep][kTile + 4], const float (&b)[kStep][kTile + 4], int ty, int tx) {
+#pragma unroll
+    for (int k = 0; k < kStep; ++k) {
+        const float4 p = *reinterpret_cast<const float4*>(&a[k][ty * 4]), q = *reinterpret_cast<const float4*>(&b[k][tx * 4]);
+        const float pv[4] = {p.x, p.y, p.z, p.w}, qv[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(pv[i], qv[j], acc[i][j]);
+    }
+}
+
+template <typename T, int GATE>
+__global__ void __launch_bounds__(kFmaThreads)
+gated_fma_kernel(const T* __restrict__ x, const T* __restrict__ w, const T* __restrict__ bias, int64_t M, int64_t C, int64_t H, T* __restrict__ h,
+                 T* __restrict__ gu) {
+    __shared__ __align__(16) float sa[kStep][kTile + 4], sg[kStep][kTile + 4], su[kStep][kTile + 4];
+    const int64_t row0 = (int64_t)blockIdx.y * kTile, col0 = (int64_t)blockIdx.x * kTile;
+    const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
+    float g[4][4] = {}, u[4][4] = {};
+    for (int64_t k0 = 0; k0 < C; k0 += kStep) {
+        stage_rows(sa, x, row0, M, k0, C);
+        stage_rows(sg, w, col0, H, k0, C);
+        stage_rows(su, w + H * C, col0, H, k0, C);
+        __syncthreads();
+        multiply(g, sa, sg, ty, tx);
+        multiply(u, sa, su, ty, tx);
+        __syncthreads();
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int64_t r = row0 + ty * 4 + i;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int64_t c = col0 + tx * 4 + j;
+            if (r >= M || c >= H) continue;
+            const float gv = g[i][j] + (bias ? to_float(bias[c]) : 0.f), uv = u[i][j] + (bias ? to_float(bias[H + c]) : 0.f);
+            put(h + r * H + c, gate_value<GATE, false>(gv) * uv);
+            if (gu) {
+                put(gu + r * 2 * H + c, gv);
+                put(gu + r * 2 * H + H + c, uv);
+            }
+        }
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kFmaThreads)
+input_grad_fma_kernel(const T* __restrict__ dgu, const T* __restrict__ w, int64_t M, int64_t C, int64_t K, T* __restrict__ dx) {
+    __shared__ __align__(16) float sa[kStep][kTile + 4], sb[kStep][kTile + 4];
+    const int64_t row0 = (int64_t)blockIdx.y * kTile, col0 = (int64_t)blockIdx.x * kTile;
+    const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
+    float acc[4][4] = {};
+    for (int64_t k0 = 0; k0 < K; k0 += kStep) {
+        stage_rows(sa, dgu, row0, M, k0, K);
+        stage_cols(sb, w, k0, K, col0, C);
+        __syncthreads();
+        multiply(acc, sa, sb, ty, tx);
+        __syncthreads();
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int64_t r = row0 + ty * 4 + i, c = col0 + tx * 4 + j;
+            if (r < M && c < C) put(dx + r * C + c, acc[i][j]);
+        }
+}
+
+// ---------------------------------------------------------------------------------------------
+// dgu = dh u f'(a) | dh f(a), and their column sums.  A warp walks down a strip of 32 * VEC columns, so that every thread keeps the sums of
+// its columns; a block's eight warps meet in shared memory, the blocks of a strip in `partial` [chunks x 2H].
+// Bound by HBM: three values read and two written for every two sums.
+// ---------------------------------------------------------------------------------------------
+constexpr int kBackThreads = 256, kBackWarps = kBackThreads / 32;
+
+template <typename T, int VEC> struct Pack;
+template <> struct Pack<uint16_t, 8> {
+    using bits = uint4;
+    static __device__ void unpack(const uint4& q, float (&v)[8]) {
+        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[2 * e] = __uint_as_float(w[e] << 16);
+            v[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
+        }
+    }
+    static __device__ uint4 pack(const float (&v)[8]) {
+        return make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+    }
+};
+template <> struct Pack<float, 4> {
+    using bits = float4;
+    static __device__ void unpack(const float4& q, float (&v)[4]) { v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w; }
+    static __device__ float4 pack(const float (&v)[4]) { return make_float4(v[0], v[1], v[2], v[3]); }
+};
+template <> struct Pack<uint16_t, 1> {
+    using bits = uint16_t;
+    static __device__ void unpack(const uint16_t& q, float (&v)[1]) { v[0] = to_float(q); }
+    static __device__ uint16_t pack(const float (&v)[1]) { return (uint16_t)pack_bf16(v[0], 0.f); }
+};
+template <> struct Pack<float, 1> {
+    using bits = float;
+    static __device__ void unpack(const float& q, float (&v)[1]) { v[0] = q; }
+    static __device__ float pack(const float (&v)[1]) { return v[0]; }
+};
+
+template <typename T, int VEC, int GATE>
+__global__ void __launch_bounds__(kBackThreads)
+gated_backward_kernel(const T* __restrict__ dh, const T* __restrict__ gu, int64_t M, int64_t H, T* __restrict__ dgu, float* __restrict__ partial) {
+    using P = Pack<T, VEC>;
+    __shared__ float sums[2][kBackWarps][32 * VEC];
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int64_t col = ((int64_t)blockIdx.x * 32 + lane) * VEC;
+    float sg[VEC] = {}, su[VEC] = {};
+    if (col < H) {
+        for (int64_t r = (int64_t)blockIdx.y * kBackWarps + warp; r < M; r += (int64_t)gridDim.y * kBackWarps) {
+            float d[VEC], a[VEC], u[VEC];
+            P::unpack(*reinterpret_cast<const typename P::bits*>(dh + r * H + col), d);
+            P::unpack(*reinterpret_cast<const typename P::bits*>(gu + r * 2 * H + col), a);
+            P::unpack(*reinterpret_cast<const typename P::bits*>(gu + r * 2 * H + H + col), u);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                float value, slope;
+                gate_value_and_slope<GATE, sizeof(T) == 2>(a[e], value, slope);
+                a[e] = d[e] * u[e] * slope;
+                u[e] = d[e] * value;
+                sg[e] += a[e];
+                su[e] += u[e];
+            }
+            *reinterpret_cast<typename P::bits*>(dgu + r * 2 * H + col) = P::pack(a);
+            *reinterpret_cast<typename P::bits*>(dgu + r * 2 * H + H + col) = P::pack(u);
+        }
+    }
+    if (!partial) return;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+        sums[0][warp][lane * VEC + e] = sg[e];
+        sums[1][warp][lane * VEC + e] = su[e];
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * 32 * VEC; i += kBackThreads) {
+        const int half = i / (32 * VEC), c = i % (32 * VEC);
+        const int64_t at = (int64_t)blockIdx.x * 32 * VEC + c;
+        if (at >= H) continue;
+        float s = 0.f;
+        for (int k = 0; k < kBackWarps; ++k) s += sums[half][k][c];
+        partial[(int64_t)blockIdx.y * 2 * H + half * H + at] = s;
+    }
+}
+
+template <typename T>
+__global__ void column_sums_kernel(const float* __restrict__ partial, int chunks, int64_t cols, T* __restrict__ db) {
+    const int64_t c = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+    if (c >= cols) return;
+    float s = 0.f;
+    for (int k = 0; k < chunks; ++k) s += partial[k * cols + c];
+    put(db + c, s);
+}
+
+int back_vec(int64_t H, dropit_dtype dtype) {
+    const int wide = dtype == DROPIT_BF16 ? 8 : 4;
+    return H % wide == 0 ? wide : 1;
+}
+// Blocks along the rows: about four blocks per SM in all.
+int64_t back_chunks(int64_t M, int64_t H, dropit_dtype dtype) {
+    const int64_t strips = (H + 32 * back_vec(H, dtype) - 1) / (32 * back_vec(H, dtype));
+    const int64_t want = (4 * (int64_t)sm_count() + strips - 1) / strips;
+    return std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want, 65535), (M + kBackWarps - 1) / kBackWarps));
+}
+
+template <typename T, int VEC>
+void launch_backward(const void* dh, const void* gu, int64_t M, int64_t H, dropit_gate gate, void* dgu, float* partial, int64_t chunks, cudaStream_t stream) {
+    const dim3 grid((unsigned)((H + 32 * VEC - 1) / (32 * VEC)), (unsigned)chunks);
+    auto kernel = gate == DROPIT_GATE_SILU ? gated_backward_kernel<T, VEC, DROPIT_GATE_SILU>
+                  : gate == DROPIT_GATE_GELU ? gated_backward_kernel<T, VEC, DROPIT_GATE_GELU> : gated_backward_kernel<T, VEC, DROPIT_GATE_RELU>;
+    kernel<<<grid, kBackThreads, 0, stream>>>((const T*)dh, (const T*)gu, M, H, (T*)dgu, partial);
+}
+
+template <typename T>
+void launch_fma(const void* x, const void* w, const void* bias, int64_t M, int64_t C, int64_t H, dropit_gate gate, void* h, void* gu, cudaStream_t stream) {
+    const dim3 grid((unsigned)((H + kTile - 1) / kTile), (unsigned)((M + kTile - 1) / kTile));
+    auto kernel = gate == DROPIT_GATE_SILU ? gated_fma_kernel<T, DROPIT_GATE_SILU>
+                  : gate == DROPIT_GATE_GELU ? gated_fma_kernel<T, DROPIT_GATE_GELU> : gated_fma_kernel<T, DROPIT_GATE_RELU>;
+    kernel<<<grid, kFmaThreads, 0, stream>>>((const T*)x, (const T*)w, (const T*)bias, M, C, H, (T*)h, (T*)gu);
+}
+
+bool gate_ok(dropit_gate g) { return g == DROPIT_GATE_SILU || g == DROPIT_GATE_GELU || g == DROPIT_GATE_RELU; }
+dropit_status sizes_ok(int64_t M, int64_t C, int64_t H, dropit_dtype dtype) {
+    const int64_t limit = (int64_t)1 << 31;
+    if (M < 0 || C < 1 || H < 1 || (dtype != DROPIT_BF16 && dtype != DROPIT_F32)) return DROPIT_ERR_INVALID_ARG;
+    if (C >= limit || 2 * H >= limit || M >= limit || M * C >= limit || M * 2 * H >= limit || 2 * H * C >= limit) return DROPIT_ERR_INVALID_ARG;
+    return DROPIT_OK;
+}
+bool buffers_ok(std::initializer_list<const void*> needed) {
+    for (const void* p : needed)
+        if (!p || !is_aligned16(p)) return false;
+    return true;
+}
+
+}  // namespace
+
+}  // namespace dropit
+
+using namespace dropit;
+
+extern "C" dropit_status dropit_gated_linear(const void* x, const void* w, const void* bias, int64_t M, int64_t C, int64_t H, dropit_dtype dtype,
+                                             dropit_gate gate, void* h, void* gu, int32_t* dev_status, void* cuda_stream) {
+    const dropit_status sizes = sizes_ok(M, C, H, dtype);
+    if (sizes != DROPIT_OK || !gate_ok(gate)) return DROPIT_ERR_INVALID_ARG;
+    if (M == 0) return DROPIT_OK;
+    if (!buffers_ok({x, w, h}) || !is_aligned16(bias) || !is_aligned16(gu)) return DROPIT_ERR_INVALID_ARG;
+    (void)dev_status;
+    if (M > (int64_t)65535 * kTile) return DROPIT_ERR_UNSUPPORTED;
+    if (dtype == DROPIT_BF16) launch_fma<uint16_t>(x, w, bias, M, C, H, gate, h, gu, as_stream(cuda_stream));
+    else launch_fma<float>(x, w, bias, M, C, H, gate, h, gu, as_stream(cuda_stream));
+    return check_launch();
+}
+
+extern "C" dropit_status dropit_gated_linear_backward_workspace(int64_t M, int64_t H, dropit_dtype dtype, size_t* workspace_bytes) {
+    if (sizes_ok(M, 1, H, dtype) != DROPIT_OK || !workspace_bytes) return DROPIT_ERR_INVALID_ARG;
+    *workspace_bytes = (size_t)back_chunks(M, H, dtype) * 2 * H * sizeof(float);
+    return DROPIT_OK;
+}
+
+extern "C" dropit_status dropit_gated_linear_backward(const void* dh, const void* gu, int64_t M, int64_t H, dropit_dtype dtype, dropit_gate gate,
+                                                      void* dgu, void* db, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    if (sizes_ok(M, 1, H, dtype) != DROPIT_OK || !gate_ok(gate)) return DROPIT_ERR_INVALID_ARG;
+    if (M == 0 && !db) return DROPIT_OK;
+    if ((M && !buffers_ok({dh, gu, dgu})) || !is_aligned16(db)) return DROPIT_ERR_INVALID_ARG;
+    const int64_t chunks = back_chunks(M, H, dtype);
+    if (db && (!workspace || !is_aligned16(workspace))) return DROPIT_ERR_INVALID_ARG;
+    if (db && workspace_bytes < (size_t)chunks * 2 * H * sizeof(float)) return DROPIT_ERR_WORKSPACE;
+    float* partial = db ? reinterpret_cast<float*>(workspace) : nullptr;
+    cudaStream_t stream = as_stream(cuda_stream);
+    const int vec = back_vec(H, dtype);
+    if (dtype == DROPIT_BF16) {
+        if (vec == 8) launch_backward<uint16_t, 8>(dh, gu, M, H, gate, dgu, partial, chunks, stream);
+        else launch_backward<uint16_t, 1>(dh, gu, M, H, gate, dgu, partial, chunks, stream);
+    } else {
+        if (vec == 4) launch_backward<float, 4>(dh, gu, M, H, gate, dgu, partial, chunks, stream);
+        else launch_backward<float, 1>(dh, gu, M, H, gate, dgu, partial, chunks, stream);
+    }
+    const dropit_status s = check_launch();
+    if (s != DROPIT_OK || !db) return s;
+    const unsigned blocks = (unsigned)((2 * H + 255) / 256);
+    if (dtype == DROPIT_BF16) column_sums_kernel<uint16_t><<<blocks, 256, 0, stream>>>(partial, (int)chunks, 2 * H, (uint16_t*)db);
+    else column_sums_kernel<float><<<blocks, 256, 0, stream>>>(partial, (int)chunks, 2 * H, (float*)db);
+    return check_launch();
+}
+
+extern "C" dropit_status dropit_gated_input_grad(const void* dgu, const void* w, int64_t M, int64_t C, int64_t H, dropit_dtype dtype, void* dx,
+                                                 int32_t* dev_status, void* cuda_stream) {
+    if (sizes_ok(M, C, H, dtype) != DROPIT_OK) return DROPIT_ERR_INVALID_ARG;
+    if (M == 0) return DROPIT_OK;
+    if (!buffers_ok({dgu, w, dx})) return DROPIT_ERR_INVALID_ARG;
+    (void)dev_status;
+    if (M > (int64_t)65535 * kTile) return DROPIT_ERR_UNSUPPORTED;
+    const dim3 grid((unsigned)((C + kTile - 1) / kTile), (unsigned)((M + kTile - 1) / kTile));
+    if (dtype == DROPIT_BF16)
+        input_grad_fma_kernel<uint16_t><<<grid, kFmaThreads, 0, as_stream(cuda_stream)>>>((const uint16_t*)dgu, (const uint16_t*)w, M, C, 2 * H, (uint16_t*)dx);
+    else
+        input_grad_fma_kernel<float><<<grid, kFmaThreads, 0, as_stream(cuda_stream)>>>((const float*)dgu, (const float*)w, M, C, 2 * H, (float*)dx);
+    return check_launch();
+}

@@ -1,10 +1,12 @@
 // Python binding of the calls that a training step makes, as a native module: argument checks, output and scratch tensors,
-// stream lookup and the autograd node of GELU + Linear in C++, on top of the C ABI in include/dropit.h.  A layer call is tens
+// stream lookup and the autograd nodes (GELU + Linear, gated linear, rotary positions) in C++, on top of the C ABI in include/dropit.h.  A layer call is tens
 // of microseconds of GPU time, less than what marshalling the same calls through ctypes takes on the host.
 #include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/extension.h>
+#include <ATen/MemoryOverlap.h>
 
 #include <mutex>
 #include <tuple>
@@ -236,6 +238,339 @@ Tensor gelu_linear(const Tensor& x, const Tensor& weight, const c10::optional<Te
     return GeluLinear::apply(x, weight, bias, gamma, fmt, table);
 }
 
+// ---- gated linear: h = f(x Wg^T + bg) * (x Wu^T + bu) ----
+
+// The library takes 16-byte aligned buffers; a slice may start anywhere.
+Tensor aligned(const Tensor& t) {
+    const Tensor c = t.contiguous();
+    return reinterpret_cast<uintptr_t>(c.data_ptr()) % 16 ? c.clone() : c;
+}
+void require_like(const Tensor& t, const Tensor& x, const char* name, const char* of) {
+    if (t.device() != x.device()) throw py::value_error(std::string(name) + " is on another device than " + of);
+    if (t.scalar_type() != x.scalar_type())
+        throw py::type_error(std::string(name) + " dtype " + type_name(t) + " != " + of + " dtype " + type_name(x));
+}
+struct GatedSizes {
+    int64_t M, C, H;
+    dropit_dtype dtype;
+};
+GatedSizes gated_sizes(const Tensor& x, const Tensor& weight, const c10::optional<Tensor>& bias) {
+    if (!x.is_cuda()) throw py::value_error("x must be a CUDA tensor (there is no CPU path)");
+    GatedSizes s;
+    s.dtype = dtype_code(x, "x");
+    if (weight.dim() != 2 || weight.size(0) % 2 || weight.size(0) == 0 || weight.size(1) == 0)
+        throw py::value_error("weight must be [2 * hidden, channels]: the gate's rows, then the other half");
+    s.C = weight.size(1);
+    s.H = weight.size(0) / 2;
+    if (x.dim() < 1 || x.size(-1) != s.C) throw py::value_error("x must have " + std::to_string(s.C) + " channels in its last dimension");
+    s.M = x.numel() / s.C;
+    require_like(weight, x, "weight", "x");
+    if (bias.has_value() && bias->defined()) {
+        require_like(*bias, x, "bias", "x");
+        if (bias->dim() != 1 || bias->numel() != 2 * s.H) throw py::value_error("bias must have " + std::to_string(2 * s.H) + " elements");
+    }
+    return s;
+}
+
+// h and, with keep, gu = a | u; both as matrices of M rows
+std::tuple<Tensor, Tensor> gated_products(const Tensor& x2, const Tensor& weight, const c10::optional<Tensor>& bias, const GatedSizes& s, int64_t gate,
+                                          bool keep) {
+    c10::cuda::CUDAGuard guard(x2.device());
+    const Tensor w = aligned(weight);
+    Tensor b;
+    if (bias.has_value() && bias->defined()) b = aligned(*bias);
+    Tensor h = at::detail::empty_cuda({s.M, s.H}, x2.scalar_type(), x2.device(), c10::nullopt), gu;
+    if (keep) gu = at::detail::empty_cuda({s.M, 2 * s.H}, x2.scalar_type(), x2.device(), c10::nullopt);
+    check(dropit_gated_linear(ptr(x2), ptr(w), b.defined() ? ptr(b) : nullptr, s.M, s.C, s.H, s.dtype, (dropit_gate)gate, ptr(h),
+                              keep ? ptr(gu) : nullptr, status_ptr(x2), current_stream(x2)), "dropit_gated_linear");
+    return {h, gu};
+}
+std::vector<int64_t> with_last(const Tensor& x, int64_t last) {
+    std::vector<int64_t> shape = x.sizes().vec();
+    shape.back() = last;
+    return shape;
+}
+
+std::tuple<Tensor, c10::optional<Tensor>> gated_linear(const Tensor& x, const Tensor& weight, const c10::optional<Tensor>& bias, int64_t gate, bool keep) {
+    const GatedSizes s = gated_sizes(x, weight, bias);
+    Tensor h, gu;
+    std::tie(h, gu) = gated_products(aligned(x.reshape({s.M, s.C})), weight, bias, s, gate, keep);
+    c10::optional<Tensor> kept;
+    if (keep) kept = gu.reshape(with_last(x, 2 * s.H));
+    return {h.reshape(with_last(x, s.H)), kept};
+}
+
+std::tuple<Tensor, c10::optional<Tensor>> gated_linear_backward(const Tensor& dh, const Tensor& gu, int64_t gate, bool want_db) {
+    if (!dh.is_cuda()) throw py::value_error("dh must be a CUDA tensor (there is no CPU path)");
+    const dropit_dtype dt = dtype_code(dh, "dh");
+    require_like(gu, dh, "gu", "dh");
+    if (dh.dim() < 1 || dh.size(-1) == 0 || gu.sizes().vec() != with_last(dh, 2 * dh.size(-1)))
+        throw py::value_error("gu must have dh's shape with twice its last dimension");
+    c10::cuda::CUDAGuard guard(dh.device());
+    const int64_t H = dh.size(-1), M = dh.numel() / H;
+    const Tensor d = aligned(dh), k = aligned(gu);
+    Tensor dgu = at::detail::empty_cuda(gu.sizes(), gu.scalar_type(), gu.device(), c10::nullopt);
+    c10::optional<Tensor> db;
+    Tensor ws;
+    if (want_db) {
+        size_t bytes;
+        check(dropit_gated_linear_backward_workspace(M, H, dt, &bytes), "dropit_gated_linear_backward_workspace");
+        db = empty1(2 * H, dh.scalar_type(), dh);
+        ws = empty1(bytes > 16 ? (int64_t)bytes : 16, at::kByte, dh);
+    }
+    check(dropit_gated_linear_backward(ptr(d), ptr(k), M, H, dt, (dropit_gate)gate, ptr(dgu), want_db ? ptr(*db) : nullptr, want_db ? ptr(ws) : nullptr,
+                                       want_db ? (size_t)ws.numel() : 0, current_stream(dh)), "dropit_gated_linear_backward");
+    return {dgu, db};
+}
+
+Tensor gated_input_grad(const Tensor& dgu, const Tensor& weight) {
+    if (!dgu.is_cuda()) throw py::value_error("dgu must be a CUDA tensor (there is no CPU path)");
+    const dropit_dtype dt = dtype_code(dgu, "dgu");
+    require_like(weight, dgu, "weight", "dgu");
+    if (weight.dim() != 2 || weight.size(0) % 2 || dgu.dim() < 1 || dgu.size(-1) != weight.size(0) || weight.numel() == 0)
+        throw py::value_error("dgu's last dimension must be weight's first, 2 * hidden");
+    c10::cuda::CUDAGuard guard(dgu.device());
+    const int64_t K = weight.size(0), C = weight.size(1), M = dgu.numel() / K;
+    const Tensor d = aligned(dgu), w = aligned(weight);
+    Tensor dx = at::detail::empty_cuda(with_last(dgu, C), dgu.scalar_type(), dgu.device(), c10::nullopt);
+    check(dropit_gated_input_grad(ptr(d), ptr(w), M, C, K / 2, dt, ptr(dx), status_ptr(dgu), current_stream(dgu)), "dropit_gated_input_grad");
+    return dx;
+}
+
+// The layer: x is cached as D(x) for the weight gradient (Sec. 3.2), a and u as the gate's own cache (Sec. 3.5).
+struct GatedLinear : public torch::autograd::Function<GatedLinear> {
+    static Tensor forward(torch::autograd::AutogradContext* ctx, const Tensor& x, const Tensor& weight, const c10::optional<Tensor>& bias,
+                          double gamma, int64_t fmt, int64_t gate) {
+        const GatedSizes s = gated_sizes(x, weight, bias);
+        const Tensor x2 = aligned(x.reshape({s.M, s.C}));
+        Tensor h, gu;
+        std::tie(h, gu) = gated_products(x2, weight, bias, s, gate, true);
+        const bool has_bias = bias.has_value() && bias->defined();
+        torch::autograd::variable_list saved{weight, gu};
+        if (weight.requires_grad()) {
+            Tensor values, meta, offsets;
+            int64_t k;
+            std::tie(values, meta, offsets, k) = compress(x2, gamma, (int)fmt, c10::nullopt);
+            saved.insert(saved.end(), {values, meta, offsets});
+            ctx->saved_data["k"] = k;
+        }
+        ctx->save_for_backward(saved);
+        ctx->saved_data["shape"] = x.sizes().vec();
+        ctx->saved_data["form"] = std::vector<int64_t>{fmt, gate, has_bias};
+        return h.reshape(with_last(x, s.H));
+    }
+    static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads) {
+        const auto saved = ctx->get_saved_variables();
+        const Tensor &weight = saved[0], &gu = saved[1];
+        const auto shape = ctx->saved_data["shape"].toIntVector(), form = ctx->saved_data["form"].toIntVector();
+        const int64_t H = gu.size(1) / 2;
+        Tensor dx, dw, db;
+        {
+            at::AutoGradMode no_graph(false);
+            const Tensor dh = grads[0].reshape({-1, H}).to(gu.scalar_type());
+            Tensor dgu;
+            c10::optional<Tensor> sums;
+            std::tie(dgu, sums) = gated_linear_backward(dh, gu, form[1], form[2] && ctx->needs_input_grad(2));
+            if (sums.has_value()) db = *sums;
+            if (ctx->needs_input_grad(0)) dx = gated_input_grad(dgu, weight).reshape(shape);
+            if (ctx->needs_input_grad(1))
+                dw = weight_grad(dgu, saved[2], saved[3], saved[4], gu.size(0) * weight.size(1), weight.size(1), ctx->saved_data["k"].toInt(),
+                                 (int)form[0], c10::nullopt, false, c10::nullopt, false).to(weight.scalar_type());
+        }
+        torch::autograd::variable_list out{dx, dw, db, Tensor(), Tensor(), Tensor()};
+        if (at::GradMode::is_enabled()) {       // a and u depend on x and W: what is kept of them cannot be differentiated again
+            torch::autograd::variable_list given;
+            std::vector<size_t> at_place;
+            for (size_t i = 0; i < 3; ++i)
+                if (out[i].defined()) given.push_back(out[i].requires_grad_(true)), at_place.push_back(i);
+            auto error = std::make_shared<torch::autograd::DelayedError>("the gradients of DropITGatedLinear cannot be differentiated again",
+                                                                         (int64_t)given.size());
+            const auto guarded = (*error)(std::move(given));
+            for (size_t i = 0; i < guarded.size(); ++i) out[at_place[i]] = guarded[i];
+        }
+        return out;
+    }
+};
+Tensor gated_layer(const Tensor& x, const Tensor& weight, const c10::optional<Tensor>& bias, double gamma, int64_t fmt, int64_t gate) {
+    return GatedLinear::apply(x, weight, bias, gamma, fmt, gate);
+}
+
+// ---- rotary positions ----
+
+// A plan travels as the bytes of the C structure in a CPU tensor.
+Tensor rotary_plan(int64_t head_dim, const std::vector<int64_t>& sections, double theta, bool shared, bool interleaved) {
+    std::vector<int> s(sections.begin(), sections.end());
+    Tensor t = at::zeros({(int64_t)sizeof(dropit_rotary_plan)}, at::kByte);
+    check(dropit_rotary_make_plan((int)head_dim, s.data(), (int)s.size(), theta, shared, interleaved, (dropit_rotary_plan*)t.data_ptr()),
+          "dropit_rotary_make_plan");
+    return t;
+}
+const dropit_rotary_plan* plan_of(const Tensor& t) {
+    if (t.device().type() != at::kCPU || t.scalar_type() != at::kByte || t.numel() != (int64_t)sizeof(dropit_rotary_plan) || !t.is_contiguous())
+        throw py::value_error("plan must be what dropit_rotary_plan returned");
+    return (const dropit_rotary_plan*)t.data_ptr();
+}
+
+// [.., length, heads, head_dim] with a batch dimension or without
+dropit_rotary_tensor rotary_tensor(const Tensor& in, Tensor& out, const dropit_rotary_plan* plan, const char* name) {
+    if ((in.dim() != 3 && in.dim() != 4) || in.size(-1) != plan->head_dim)
+        throw py::value_error(std::string(name) + " must be [batch, length, heads, " + std::to_string(plan->head_dim) + "] or [length, heads, " +
+                              std::to_string(plan->head_dim) + "]");
+    const bool batched = in.dim() == 4;
+    dropit_rotary_tensor t;
+    t.in = in.numel() ? in.data_ptr() : nullptr;
+    t.out = out.numel() ? out.data_ptr() : nullptr;
+    t.in_batch = batched ? in.stride(0) : 0;
+    t.in_token = in.stride(-3);
+    t.in_head = in.stride(-2);
+    t.out_batch = batched ? out.stride(0) : 0;
+    t.out_token = out.stride(-3);
+    t.out_head = out.stride(-2);
+    t.heads = (int32_t)in.size(-2);
+    return t;
+}
+Tensor rotary_input(const Tensor& t) { return t.dim() && t.stride(-1) != 1 ? t.contiguous() : t; }
+
+std::tuple<Tensor, c10::optional<Tensor>> rotary(const Tensor& q_in, const c10::optional<Tensor>& k_in, const Tensor& positions, const Tensor& plan_bytes,
+                                                 bool inverse, bool in_place) {
+    const dropit_rotary_plan* plan = plan_of(plan_bytes);
+    if (!q_in.is_cuda()) throw py::value_error("q must be a CUDA tensor (there is no CPU path)");
+    const dropit_dtype dt = dtype_code(q_in, "q");
+    const bool has_k = k_in.has_value() && k_in->defined();
+    if (in_place && ((q_in.dim() && q_in.stride(-1) != 1) || (has_k && k_in->dim() && k_in->stride(-1) != 1)))
+        throw py::value_error("in place: the channels of a head must lie together");
+    if (in_place && (at::has_internal_overlap(q_in) == at::MemOverlap::Yes || (has_k && at::has_internal_overlap(*k_in) == at::MemOverlap::Yes)))
+        throw py::value_error("in place: an expanded tensor has no place of its own");
+    const Tensor q = rotary_input(q_in), k = has_k ? rotary_input(*k_in) : Tensor();
+    c10::cuda::CUDAGuard guard(q.device());
+    Tensor q_out = in_place ? q : Tensor(at::detail::empty_cuda(q.sizes(), q.scalar_type(), q.device(), c10::nullopt)), k_out;
+    const dropit_rotary_tensor tq = rotary_tensor(q, q_out, plan, "q");
+    dropit_rotary_tensor tk;
+    if (has_k) {
+        require_like(k, q, "k", "q");
+        k_out = in_place ? k : Tensor(at::detail::empty_cuda(k.sizes(), k.scalar_type(), k.device(), c10::nullopt));
+        tk = rotary_tensor(k, k_out, plan, "k");
+        if (k.dim() != q.dim() || k.size(-3) != q.size(-3) || (q.dim() == 4 && k.size(0) != q.size(0)))
+            throw py::value_error("k must have q's batch and length");
+    }
+    const int64_t batch = q.dim() == 4 ? q.size(0) : 1, length = q.size(-3);
+    if (positions.device() != q.device()) throw py::value_error("positions is on another device than q");
+    dropit_position_type type;
+    if (positions.scalar_type() == at::kInt) type = DROPIT_POSITION_I32;
+    else if (positions.scalar_type() == at::kLong) type = DROPIT_POSITION_I64;
+    else if (positions.scalar_type() == at::kFloat) type = DROPIT_POSITION_F32;
+    else throw py::type_error("positions: dtype " + type_name(positions) + " is not supported (int32, int64 or fp32)");
+    const bool each = positions.dim() == 3 && q.dim() == 4;
+    if ((positions.dim() != 2 && !each) || positions.size(-1) != plan->axes || positions.size(-2) != length ||
+        (each && positions.size(0) != batch && positions.size(0) != 1))
+        throw py::value_error("positions must be [length, " + std::to_string(plan->axes) + "] or [batch, length, " + std::to_string(plan->axes) +
+                              "] with q's length and batch");
+    const int64_t pos_batch = each && positions.size(0) != 1 ? positions.stride(0) : 0;
+    check(dropit_rotary(plan, batch, length, &tq, has_k ? &tk : nullptr, positions.numel() ? positions.data_ptr() : nullptr, type, pos_batch,
+                        positions.stride(-2), positions.stride(-1), dt, inverse, current_stream(q)), "dropit_rotary");
+    if (in_place) {
+        q_out.unsafeGetTensorImpl()->bump_version();
+        if (has_k) k_out.unsafeGetTensorImpl()->bump_version();
+    }
+    c10::optional<Tensor> second;
+    if (has_k) second = k_out;
+    return {q_out, second};
+}
+
+// The gradient of a rotation is the inverse rotation, which can be differentiated again.
+struct Rotary : public torch::autograd::Function<Rotary> {
+    static torch::autograd::variable_list forward(torch::autograd::AutogradContext* ctx, const Tensor& q, const c10::optional<Tensor>& k,
+                                                  const Tensor& positions, const Tensor& plan, bool inverse) {
+        ctx->save_for_backward({positions});
+        ctx->saved_data["plan"] = plan;
+        ctx->saved_data["inverse"] = inverse;
+        ctx->saved_data["k"] = k.has_value() && k->defined();
+        Tensor q_out;
+        c10::optional<Tensor> k_out;
+        std::tie(q_out, k_out) = rotary(q, k, positions, plan, inverse, false);
+        if (k_out.has_value()) return {q_out, *k_out};
+        return {q_out};
+    }
+    static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads) {
+        const auto saved = ctx->get_saved_variables();
+        const Tensor plan = ctx->saved_data["plan"].toTensor();
+        const bool inverse = !ctx->saved_data["inverse"].toBool(), has_k = ctx->saved_data["k"].toBool();
+        c10::optional<Tensor> dk;
+        if (has_k) dk = grads[1];
+        const auto out = Rotary::apply(grads[0], dk, saved[0], plan, inverse);
+        return {out[0], has_k ? out[1] : Tensor(), Tensor(), Tensor(), Tensor()};
+    }
+};
+std::tuple<Tensor, c10::optional<Tensor>> rotary_layer(const Tensor& q, const c10::optional<Tensor>& k, const Tensor& positions, const Tensor& plan,
+                                                       bool inverse) {
+    const auto out = Rotary::apply(q, k, positions, plan, inverse);
+    c10::optional<Tensor> second;
+    if (out.size() > 1) second = out[1];
+    return {out[0], second};
+}
+
+// ---- AdamW ----
+
+// The parameters that an optimizer steps, where their moments lie, and which group's settings hold for them.
+struct AdamWParams {
+    std::vector<Tensor> params;
+    std::vector<int64_t> first_block, group;
+    std::vector<std::vector<int64_t>> sizes, strides;       // as they were when the moments were laid out
+};
+using AdamWGroupTuple = std::tuple<double, c10::optional<Tensor>, double, double, double, double>;     // lr, lr on the device, decay, betas, eps
+
+// One call of the library for each combination of types and of betas and eps among the parameters that have a gradient.
+void adamw_step(const AdamWParams& all, const std::vector<AdamWGroupTuple>& settings, int64_t state_bits, bool dither, int64_t seed, const Tensor& exp_avg,
+                const Tensor& exp_avg_sq, const c10::optional<Tensor>& exp_avg_scale, const c10::optional<Tensor>& exp_avg_sq_scale,
+                const c10::optional<Tensor>& master, const Tensor& steps, const Tensor& ticket, const c10::optional<Tensor>& grad_factor) {
+    struct Call {
+        dropit_adamw_options options;
+        std::vector<dropit_adamw_tensor> tensors;
+    };
+    std::vector<Call> calls;
+    std::vector<Tensor> held;               // gradients laid out again
+    c10::cuda::CUDAGuard guard(exp_avg.device());
+    for (size_t i = 0; i < all.params.size(); ++i) {
+        const Tensor& p = all.params[i];
+        Tensor g = p.grad();
+        if (!g.defined()) continue;
+        if (g.layout() != at::kStrided) throw py::type_error("sparse gradients are not supported");
+        const dropit_dtype pt = dtype_code(p, "parameter"), gt = dtype_code(g, "gradient");
+        if (p.device() != exp_avg.device()) throw py::value_error("a parameter has moved to another device than its moments");
+        if (p.sizes() != all.sizes[i] || p.strides() != all.strides[i]) throw py::value_error("a parameter's shape or strides have changed since its moments were laid out");
+        if (g.device() != p.device() || g.sizes() != p.sizes()) throw py::value_error("a gradient differs from its parameter in shape or device");
+        if (!(p.is_contiguous() && g.is_contiguous()) && g.strides() != p.strides()) {
+            Tensor same = at::empty_strided(p.sizes(), p.strides(), g.options());
+            same.copy_(g);
+            held.push_back(same);
+            g = same;
+        }
+        double lr, decay, beta1, beta2, eps;
+        c10::optional<Tensor> lr_device;
+        std::tie(lr, lr_device, decay, beta1, beta2, eps) = settings[all.group[i]];
+        Call* call = nullptr;
+        for (Call& c : calls)
+            if (c.options.param_dtype == pt && c.options.grad_dtype == gt && c.options.beta1 == beta1 && c.options.beta2 == beta2 && c.options.eps == eps)
+                call = &c;
+        if (!call) {
+            calls.push_back({{pt, gt, (int32_t)state_bits, dither ? 1 : 0, beta1, beta2, eps, (uint32_t)seed}, {}});
+            call = &calls.back();
+            call->tensors.reserve(all.params.size());
+        }
+        call->tensors.push_back({p.data_ptr(), g.data_ptr(), lr_device.has_value() ? lr_device->data_ptr<float>() : nullptr, p.numel(),
+                                 all.first_block[i], (int32_t)i, (float)lr, (float)decay});
+    }
+    auto words = [](const c10::optional<Tensor>& t) { return t.has_value() ? t->data_ptr<float>() : nullptr; };
+    for (Call& c : calls) {
+        const dropit_adamw_state state = {exp_avg.data_ptr(), exp_avg_sq.data_ptr(), words(exp_avg_scale), words(exp_avg_sq_scale),
+                                          c.options.param_dtype == DROPIT_BF16 ? words(master) : nullptr, steps.data_ptr<int32_t>(),
+                                          (uint32_t*)ticket.data_ptr(), words(grad_factor)};
+        check(dropit_adamw_step(c.tensors.data(), (int)c.tensors.size(), &c.options, &state, current_stream(exp_avg)), "dropit_adamw_step");
+    }
+    for (size_t i = 0; i < all.params.size(); ++i)
+        if (all.params[i].grad().defined()) all.params[i].unsafeGetTensorImpl()->bump_version();
+}
+
 }  // namespace
 
 PYBIND11_MODULE(_native, m) {
@@ -255,4 +590,17 @@ PYBIND11_MODULE(_native, m) {
     m.def("weight_grad", torch::wrap_pybind_function_no_gil(weight_grad));
     m.def("conv_weight_grad", torch::wrap_pybind_function_no_gil(conv_weight_grad));
     m.def("gelu_linear", torch::wrap_pybind_function_no_gil(gelu_linear));
+    m.def("gated_linear", torch::wrap_pybind_function_no_gil(gated_linear));
+    m.def("gated_linear_backward", torch::wrap_pybind_function_no_gil(gated_linear_backward));
+    m.def("gated_input_grad", torch::wrap_pybind_function_no_gil(gated_input_grad));
+    m.def("gated_layer", torch::wrap_pybind_function_no_gil(gated_layer));
+    m.def("rotary_plan", torch::wrap_pybind_function_no_gil(rotary_plan));
+    m.def("rotary", torch::wrap_pybind_function_no_gil(rotary));
+    m.def("rotary_layer", torch::wrap_pybind_function_no_gil(rotary_layer));
+    py::class_<AdamWParams>(m, "AdamWParams").def(py::init([](std::vector<Tensor> params, std::vector<int64_t> first_block, std::vector<int64_t> group) {
+        AdamWParams all{std::move(params), std::move(first_block), std::move(group), {}, {}};
+        for (const Tensor& p : all.params) all.sizes.push_back(p.sizes().vec()), all.strides.push_back(p.strides().vec());
+        return all;
+    }));
+    m.def("adamw_step", torch::wrap_pybind_function_no_gil(adamw_step));
 }

@@ -1,0 +1,248 @@
+// Rotary positions with several axes (rows and columns of an image; time, height and width of a video) on queries and keys.
+// Pair j of a head turns by p[axis(j)] * theta^e(j): (a, b) -> (a cos - b sin, a sin + b cos); the gradient is the same with -sin.
+//
+// The angle is formed in turns: a whole-number position times the pair's turns per position as a 64-bit binary fraction, wrapping.
+// The product's high word is the angle's place within its turn, exact to 2^-32 for positions up to 2^31, where an fp32 product has
+// lost every digit (2^24 steps of one radian are known to a radian).  Positions that are fp32 take the product in 64-bit floats.
+//
+// Bound by HBM: every value is read and written once.  The angles of a block's tokens are formed once, in shared memory, and
+// serve all heads of queries and keys; one launch does both.
+#include <math.h>
+
+#include <algorithm>
+
+#include "common.cuh"
+
+namespace dropit {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kMaxAngles = 2048;            // angles of one block's tokens: 16 KB of shared memory
+
+struct RotaryTensor {
+    const void* in;
+    void* out;
+    int64_t in_batch, in_token, in_head, out_batch, out_token, out_head;
+    int heads;
+};
+struct RotaryArgs {
+    RotaryTensor t[2];                      // queries, keys
+    const void* positions;
+    int64_t pos_batch, pos_token, pos_axis;
+    int64_t tokens;                         // batch * length
+    int length, head_dim, tokens_per_block;
+    float sign;                             // -1: the inverse rotation
+    dropit_position_type position_type;
+    dropit_rotary_plan plan;
+};
+
+template <int BYTES> struct Bits;
+template <> struct Bits<2> { using type = uint16_t; };
+template <> struct Bits<4> { using type = uint32_t; };
+template <> struct Bits<8> { using type = uint2; };
+template <> struct Bits<16> { using type = uint4; };
+
+template <typename T, int N>
+struct Values {
+    union {
+        typename Bits<N * sizeof(T)>::type bits;
+        T v[N];
+    };
+    __device__ Values() {}
+};
+__device__ __forceinline__ float to_float(uint16_t b) { return __uint_as_float((uint32_t)b << 16); }
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ void from_float(float v, uint16_t& out) {
+    uint16_t r;
+    asm("cvt.rn.bf16.f32 %0, %1;" : "=h"(r) : "f"(v));
+    out = r;
+}
+__device__ __forceinline__ void from_float(float v, float& out) { out = v; }
+
+// The angle in half turns, within [-1, 1].
+__device__ __forceinline__ float half_turns(const RotaryArgs& a, int64_t offset, int pair) {
+    const int64_t at = offset + a.plan.axis[pair] * a.pos_axis;
+    const uint64_t turns = a.plan.turns[pair];
+    if (a.position_type == DROPIT_POSITION_F32) {
+        const double t = (double)reinterpret_cast<const float*>(a.positions)[at] * ((double)turns * 0x1p-64);
+        return (float)(2.0 * (t - rint(t)));
+    }
+    const int64_t p = a.position_type == DROPIT_POSITION_I64 ? reinterpret_cast<const int64_t*>(a.positions)[at]
+                                                            : (int64_t)reinterpret_cast<const int32_t*>(a.positions)[at];
+    return (float)(int32_t)(((uint64_t)p * turns) >> 32) * 0x1p-31f;
+}
+
+// A unit is VP pairs of one head (two vectors of VP values), or VP of the values behind the rotated ones, which are copied.
+template <typename T, int VP, bool INTERLEAVED>
+__global__ void __launch_bounds__(kThreads)
+rotary_kernel(const __grid_constant__ RotaryArgs a) {
+    __shared__ float2 angles[kMaxAngles];
+    const int pairs = a.plan.pairs;
+    const int64_t first = (int64_t)blockIdx.x * a.tokens_per_block;
+    const int tokens = (int)min((int64_t)a.tokens_per_block, a.tokens - first);
+    for (int i = threadIdx.x; i < tokens * pairs; i += kThreads) {
+        const int64_t token = first + i / pairs;
+        const int64_t batch = token / a.length;
+        float2 cs;
+        sincospif(half_turns(a, batch * a.pos_batch + (token - batch * a.length) * a.pos_token, i % pairs), &cs.y, &cs.x);
+        cs.y *= a.sign;
+        angles[i] = cs;
+    }
+    __syncthreads();
+    const int rotating = pairs / VP;
+    const int units = rotating + (a.head_dim - 2 * pairs) / VP;
+    const int heads = a.t[0].heads + a.t[1].heads;
+    const int total = tokens * heads * units;
+    for (int i = threadIdx.x; i < total; i += kThreads) {
+        const int row = i / units, unit = i - row * units;
+        const int local = row / heads;
+        int head = row - local * heads;
+        const int64_t token = first + local;
+        const int64_t batch = token / a.length, at = token - batch * a.length;
+        const int which = head >= a.t[0].heads;
+        const RotaryTensor& t = a.t[which];
+        if (which) head -= a.t[0].heads;
+        const T* in = reinterpret_cast<const T*>(t.in) + batch * t.in_batch + at * t.in_token + head * t.in_head;
+        T* out = reinterpret_cast<T*>(t.out) + batch * t.out_batch + at * t.out_token + head * t.out_head;
+        using Vec = Values<T, VP>;
+        using B = typename Bits<VP * sizeof(T)>::type;
+        if (unit >= rotating) {
+            const int c = 2 * pairs + (unit - rotating) * VP;
+            *reinterpret_cast<B*>(out + c) = *reinterpret_cast<const B*>(in + c);
+            continue;
+        }
+        const int c0 = INTERLEAVED ? 2 * unit * VP : unit * VP;
+        const int c1 = INTERLEAVED ? c0 + VP : pairs + c0;
+        Vec x, y;
+        x.bits = *reinterpret_cast<const B*>(in + c0);
+        y.bits = *reinterpret_cast<const B*>(in + c1);
+        const float2* cs = angles + local * pairs + unit * VP;
+#pragma unroll
+        for (int e = 0; e < VP; ++e) {
+            // halves: pair e is (x[e], y[e]); neighbours: values 2e and 2e + 1 of x followed by y
+            T& one = INTERLEAVED ? (2 * e < VP ? x.v[2 * e % VP] : y.v[2 * e % VP]) : x.v[e];
+            T& two = INTERLEAVED ? (2 * e + 1 < VP ? x.v[(2 * e + 1) % VP] : y.v[(2 * e + 1) % VP]) : y.v[e];
+            const float u = to_float(one), v = to_float(two);
+            from_float(u * cs[e].x - v * cs[e].y, one);
+            from_float(u * cs[e].y + v * cs[e].x, two);
+        }
+        *reinterpret_cast<B*>(out + c0) = x.bits;
+        *reinterpret_cast<B*>(out + c1) = y.bits;
+    }
+}
+
+template <typename T, int VP>
+void launch(const RotaryArgs& a, unsigned blocks, cudaStream_t stream) {
+    if (a.plan.interleaved) rotary_kernel<T, VP, true><<<blocks, kThreads, 0, stream>>>(a);
+    else rotary_kernel<T, VP, false><<<blocks, kThreads, 0, stream>>>(a);
+}
+
+// Whether vectors of `n` values of `size` bytes fit everywhere.
+bool takes(const RotaryArgs& a, int n, int size) {
+    if (a.plan.pairs % n || a.head_dim % n) return false;
+    for (const RotaryTensor& t : a.t) {
+        if (!t.heads) continue;
+        const uintptr_t base = reinterpret_cast<uintptr_t>(t.in) | reinterpret_cast<uintptr_t>(t.out);
+        const int64_t strides = t.in_batch | t.in_token | t.in_head | t.out_batch | t.out_token | t.out_head;
+        if (base % (uintptr_t)(n * size) || strides % n) return false;
+    }
+    return true;
+}
+
+}  // namespace
+
+}  // namespace dropit
+
+using namespace dropit;
+
+extern "C" dropit_status dropit_rotary_make_plan(int head_dim, const int* sections, int axes, double theta, int shared, int interleaved,
+                                                 dropit_rotary_plan* plan) {
+    if (!plan || !sections || axes < 1 || axes > DROPIT_ROTARY_MAX_AXES || head_dim < 2 || !(theta >= 1) || !isfinite(theta))
+        return DROPIT_ERR_INVALID_ARG;
+    int64_t rotated = 0;
+    for (int s = 0; s < axes; ++s) {
+        if (sections[s] < 0 || sections[s] % 2) return DROPIT_ERR_INVALID_ARG;
+        rotated += sections[s];
+    }
+    if (rotated < 2 || rotated > head_dim) return DROPIT_ERR_INVALID_ARG;
+    if (rotated > 2 * DROPIT_ROTARY_MAX_PAIRS) return DROPIT_ERR_UNSUPPORTED;
+    plan->head_dim = head_dim;
+    plan->pairs = (int)(rotated / 2);
+    plan->axes = axes;
+    plan->interleaved = interleaved != 0;
+    int j = 0;
+    for (int s = 0; s < axes; ++s) {
+        for (int i = 0; i < sections[s] / 2; ++i, ++j) {
+            const double exponent = shared ? 2.0 * j / (double)rotated : 2.0 * i / (double)sections[s];
+            // Turns per position, at most 1 / (2 pi), as a fraction of 2^64.
+            const long double part = powl((long double)theta, -(long double)exponent) / 6.283185307179586476925286766559L;
+            const long double high = floorl(part * 0x1p32L), low = floorl((part * 0x1p32L - high) * 0x1p32L + 0.5L);
+            plan->turns[j] = ((uint64_t)high << 32) + (uint64_t)low;
+            plan->axis[j] = (uint8_t)s;
+        }
+    }
+    for (; j < DROPIT_ROTARY_MAX_PAIRS; ++j) plan->turns[j] = 0, plan->axis[j] = 0;
+    return DROPIT_OK;
+}
+
+extern "C" dropit_status dropit_rotary(const dropit_rotary_plan* plan, int64_t batch, int64_t length, const dropit_rotary_tensor* q,
+                                       const dropit_rotary_tensor* k, const void* positions, dropit_position_type position_type,
+                                       int64_t pos_batch, int64_t pos_token, int64_t pos_axis, dropit_dtype dtype, int inverse,
+                                       void* cuda_stream) {
+    if (!plan || !q || batch < 0 || length < 0 || length > INT32_MAX) return DROPIT_ERR_INVALID_ARG;
+    if (plan->pairs < 1 || plan->pairs > DROPIT_ROTARY_MAX_PAIRS || plan->head_dim < 2 * plan->pairs) return DROPIT_ERR_INVALID_ARG;
+    if (dtype != DROPIT_BF16 && dtype != DROPIT_F32) return DROPIT_ERR_INVALID_ARG;
+    if (position_type != DROPIT_POSITION_I32 && position_type != DROPIT_POSITION_I64 && position_type != DROPIT_POSITION_F32)
+        return DROPIT_ERR_INVALID_ARG;
+    const int size = dtype == DROPIT_BF16 ? 2 : 4;
+    RotaryArgs a = {};
+    int64_t heads = 0;
+    for (int i = 0; i < 2; ++i) {
+        const dropit_rotary_tensor* t = i ? k : q;
+        if (!t) continue;
+        if (t->heads < 0) return DROPIT_ERR_INVALID_ARG;
+        heads += t->heads;
+        a.t[i] = {t->in, t->out, t->in_batch, t->in_token, t->in_head, t->out_batch, t->out_token, t->out_head, t->heads};
+        if (t->heads && batch && length &&
+            (!t->in || !t->out || (reinterpret_cast<uintptr_t>(t->in) | reinterpret_cast<uintptr_t>(t->out)) % (uintptr_t)size))
+            return DROPIT_ERR_INVALID_ARG;
+    }
+    if (length && batch > INT64_MAX / length) return DROPIT_ERR_INVALID_ARG;
+    const int64_t tokens = batch * length;
+    if (tokens == 0 || heads == 0) return DROPIT_OK;
+    if (!positions || reinterpret_cast<uintptr_t>(positions) % (position_type == DROPIT_POSITION_I64 ? 8 : 4)) return DROPIT_ERR_INVALID_ARG;
+    if (heads * plan->head_dim > (1 << 20)) return DROPIT_ERR_UNSUPPORTED;      // a block's work is counted in 32 bits
+    a.positions = positions;
+    a.pos_batch = pos_batch;
+    a.pos_token = pos_token;
+    a.pos_axis = pos_axis;
+    a.tokens = tokens;
+    a.length = (int)length;
+    a.head_dim = plan->head_dim;
+    a.sign = inverse ? -1.f : 1.f;
+    a.position_type = position_type;
+    a.plan = *plan;
+    // Vectors of 16 bytes, else of 8, else single values.
+    int vec = 1;
+    for (int n = 16 / size; n >= 4; n /= 2)
+        if (takes(a, n, size)) { vec = n; break; }
+    // Four units a thread, as far as the angles fit and every SM has blocks.
+    const int64_t units = heads * ((plan->head_dim - plan->pairs) / vec);
+    int64_t per_block = (4 * kThreads + units - 1) / units;
+    per_block = std::min<int64_t>(per_block, kMaxAngles / plan->pairs);
+    per_block = std::min<int64_t>(per_block, std::max<int64_t>(1, tokens / (2 * sm_count())));
+    a.tokens_per_block = (int)std::max<int64_t>(1, per_block);
+    const int64_t blocks = (tokens + a.tokens_per_block - 1) / a.tokens_per_block;
+    if (blocks > INT32_MAX) return DROPIT_ERR_UNSUPPORTED;
+    cudaStream_t stream = as_stream(cuda_stream);
+    if (dtype == DROPIT_BF16) {
+        if (vec == 8) launch<uint16_t, 8>(a, (unsigned)blocks, stream);
+        else if (vec == 4) launch<uint16_t, 4>(a, (unsigned)blocks, stream);
+        else launch<uint16_t, 1>(a, (unsigned)blocks, stream);
+    } else {
+        if (vec == 4) launch<float, 4>(a, (unsigned)blocks, stream);
+        else launch<float, 1>(a, (unsigned)blocks, stream);
+    }
+    return check_launch();
+}

@@ -195,6 +195,67 @@ class DropITGeluLinear(nn.Linear):
         return DropITGeluLinearFn.apply(x, self.weight, self.bias, self.gamma, self.fmt)
 
 
+class DropITGatedLinear(nn.Module):
+    """The first half of a gated feed-forward block, h = f(x Wg^T + bg) * (x Wu^T + bu), with the layer input cached as D(x): both
+    products, the gate function f ("silu", "gelu" or "relu") and their product are one kernel.  The two projections are one parameter
+    `weight` [2 * hidden, channels] (`bias` [2 * hidden]), the gate's half first.  The gate keeps its own cache, the two projections
+    (Sec. 3.5); their gradients with respect to W come from D(x) (Eq. 6), with respect to x from W alone (Eq. 3).  The gradients cannot be
+    differentiated again."""
+
+    def __init__(self, in_features: int, hidden_features: int, bias: bool = True, gate: str = "silu", gamma: float = 0.9,
+                 fmt: str = "bitmask", device=None, dtype=None):
+        super().__init__()
+        self.in_features, self.hidden_features = int(in_features), int(hidden_features)
+        self._gate = api._gate_code(gate)
+        self._fmt = api._FMT_CODE[fmt]
+        self.gate, self.gamma, self.fmt = gate, float(gamma), fmt
+        self.weight = nn.Parameter(torch.empty(2 * self.hidden_features, self.in_features, device=device, dtype=dtype))
+        self.bias = nn.Parameter(torch.empty(2 * self.hidden_features, device=device, dtype=dtype)) if bias else None
+        self.reset_parameters()
+
+    def reset_parameters(self):
+        """As nn.Linear's."""
+        nn.init.kaiming_uniform_(self.weight, a=5 ** 0.5)
+        if self.bias is not None:
+            bound = self.in_features ** -0.5
+            nn.init.uniform_(self.bias, -bound, bound)
+
+    def extra_repr(self) -> str:
+        return "in_features=%d, hidden_features=%d, bias=%s, gate=%s, gamma=%g" % (
+            self.in_features, self.hidden_features, self.bias is not None, self.gate, self.gamma)
+
+    def forward(self, x):
+        weight, bias = self.weight, self.bias
+        if torch.is_autocast_enabled("cuda"):      # the type that a Linear would run in
+            dt = torch.get_autocast_dtype("cuda")
+            x, weight, bias = x.to(dt), weight.to(dt), None if bias is None else bias.to(dt)
+        if not (self.training and torch.is_grad_enabled()):
+            if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or (bias is not None and bias.requires_grad)):
+                # gradients outside of training are those of the stock operations (Sec. 3.5: inference is unchanged)
+                a, u = F.linear(x, weight, bias).chunk(2, -1)
+                return {"silu": F.silu, "gelu": F.gelu, "relu": F.relu}[self.gate](a) * u
+            return api._native().gated_linear(x, weight, bias, self._gate, False)[0]
+        return api._native().gated_layer(x, weight, bias, self.gamma, self._fmt, self._gate)
+
+
+class DropITRotary(nn.Module):
+    """Rotary positions with several axes on queries and keys (see api.dropit_rotary and dropit_rotary_plan): (q, k, positions) ->
+    (q', k').  The backward pass is the inverse rotation and keeps the positions only."""
+
+    def __init__(self, head_dim: int, sections, theta: float = 10000.0, interleaved: bool = False, shared: bool = False):
+        super().__init__()
+        self.head_dim, self.sections, self.theta = int(head_dim), tuple(int(s) for s in sections), float(theta)
+        self.interleaved, self.shared = bool(interleaved), bool(shared)
+        self._plan = api.dropit_rotary_plan(head_dim, sections, theta, interleaved, shared)
+
+    def extra_repr(self) -> str:
+        return "head_dim=%d, sections=%s, theta=%g, interleaved=%s, shared=%s" % (
+            self.head_dim, self.sections, self.theta, self.interleaved, self.shared)
+
+    def forward(self, q, k, positions):
+        return api._native().rotary_layer(q, k, positions, self._plan, False)
+
+
 class DropITConv2d(nn.Conv2d, _Strategy):
     """nn.Conv2d (groups 1, dilation 1, square stride/padding) with a compressed input cache."""
 
