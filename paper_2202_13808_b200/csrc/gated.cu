@@ -251,7 +251,7 @@ extern "C" dropit_status dropit_gated_linear(const void* x, const void* w, const
     if (sizes != DROPIT_OK || !gate_ok(gate)) return DROPIT_ERR_INVALID_ARG;
     if (M == 0) return DROPIT_OK;
     if (!buffers_ok({x, w, h}) || !is_aligned16(bias) || !is_aligned16(gu)) return DROPIT_ERR_INVALID_ARG;
-    (void)dev_status;
+    if (dtype == DROPIT_BF16 && gated_tc_takes(M, C, H)) return gated_tc_forward(x, w, bias, M, C, H, gate, h, gu, dev_status, as_stream(cuda_stream));
     if (M > (int64_t)65535 * kTile) return DROPIT_ERR_UNSUPPORTED;
     if (dtype == DROPIT_BF16) launch_fma<uint16_t>(x, w, bias, M, C, H, gate, h, gu, as_stream(cuda_stream));
     else launch_fma<float>(x, w, bias, M, C, H, gate, h, gu, as_stream(cuda_stream));
@@ -295,7 +295,7 @@ extern "C" dropit_status dropit_gated_input_grad(const void* dgu, const void* w,
     if (sizes_ok(M, C, H, dtype) != DROPIT_OK) return DROPIT_ERR_INVALID_ARG;
     if (M == 0) return DROPIT_OK;
     if (!buffers_ok({dgu, w, dx})) return DROPIT_ERR_INVALID_ARG;
-    (void)dev_status;
+    if (dtype == DROPIT_BF16 && gated_tc_takes(M, C, H)) return gated_tc_input_grad(dgu, w, M, C, H, dx, dev_status, as_stream(cuda_stream));
     if (M > (int64_t)65535 * kTile) return DROPIT_ERR_UNSUPPORTED;
     const dim3 grid((unsigned)((C + kTile - 1) / kTile), (unsigned)((M + kTile - 1) / kTile));
     if (dtype == DROPIT_BF16)

@@ -33,4 +33,10 @@ __device__ __forceinline__ void gate_value_and_slope(float a, float& value, floa
     }
 }
 
+// Tensor-core forms (bf16, C and H multiples of 8): false if the sizes are not theirs.
+bool gated_tc_takes(int64_t M, int64_t C, int64_t H);
+dropit_status gated_tc_forward(const void* x, const void* w, const void* bias, int64_t M, int64_t C, int64_t H, dropit_gate gate, void* h, void* gu,
+                               int32_t* dev_status, cudaStream_t stream);
+dropit_status gated_tc_input_grad(const void* dgu, const void* w, int64_t M, int64_t C, int64_t H, void* dx, int32_t* dev_status, cudaStream_t stream);
+
 }  // namespace dropit
