@@ -60,89 +60,98 @@ struct Args {
 static_assert(sizeof(Args) <= 32764, "kernel arguments");
 
 // A mixing function of 32-bit words: two multiplications, three shifts (the constants are those of C. Wellons' published search for low bias).
-__host__ __device__ __forceinline__ uint32_t mix(uint32_t x) {
-    x ^= x >> 16;
+__host__ __device__ __forceinline__ uint32_t mix_rest(uint32_t x) {       // all but its first line
     x *= 0x7FEB352Du;
     x ^= x >> 15;
     x *= 0x846CA68Bu;
     return x ^ (x >> 16);
 }
+__host__ __device__ __forceinline__ uint32_t mix(uint32_t x) { return mix_rest(x ^ (x >> 16)); }
 
-// Four values at p + at, of which the tensor has `left`.
-__device__ __forceinline__ void load4(const float* p, int64_t at, int left, bool vec, float (&v)[4]) {
-    if (vec && left >= 4) {
+// ---- four values of a lane, FULL: all inside the tensor and aligned ----
+template <bool FULL>
+__device__ __forceinline__ void load4(const float* p, int64_t at, int64_t n, float (&v)[4]) {
+    if constexpr (FULL) {
         const float4 q = *reinterpret_cast<const float4*>(p + at);
         v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
-        return;
-    }
+    } else {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = e < left ? p[at + e] : 0.f;
+        for (int e = 0; e < 4; ++e) v[e] = at + e < n ? p[at + e] : 0.f;
+    }
 }
-__device__ __forceinline__ float bf16_value(uint32_t b) { return __uint_as_float(b << 16); }
-__device__ __forceinline__ void load4(const uint16_t* p, int64_t at, int left, bool vec, float (&v)[4]) {
-    if (vec && left >= 4) {
+template <bool FULL>
+__device__ __forceinline__ void load4(const uint16_t* p, int64_t at, int64_t n, float (&v)[4]) {
+    if constexpr (FULL) {
         const uint2 q = *reinterpret_cast<const uint2*>(p + at);
-        v[0] = bf16_value(q.x & 0xFFFFu); v[1] = bf16_value(q.x >> 16); v[2] = bf16_value(q.y & 0xFFFFu); v[3] = bf16_value(q.y >> 16);
-        return;
-    }
+        v[0] = __uint_as_float(q.x << 16); v[1] = __uint_as_float(q.x & 0xFFFF0000u);
+        v[2] = __uint_as_float(q.y << 16); v[3] = __uint_as_float(q.y & 0xFFFF0000u);
+    } else {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = e < left ? bf16_value(p[at + e]) : 0.f;
+        for (int e = 0; e < 4; ++e) v[e] = at + e < n ? __uint_as_float((uint32_t)p[at + e] << 16) : 0.f;
+    }
 }
-__device__ __forceinline__ void store4(float* p, int64_t at, int left, bool vec, const float (&v)[4], const uint32_t (&)[4], bool) {
-    if (vec && left >= 4) {
+template <bool FULL>
+__device__ __forceinline__ void store4(float* p, int64_t at, int64_t n, const float (&v)[4]) {
+    if constexpr (FULL) {
         *reinterpret_cast<float4*>(p + at) = make_float4(v[0], v[1], v[2], v[3]);
-        return;
-    }
+    } else {
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-        if (e < left) p[at + e] = v[e];
+        for (int e = 0; e < 4; ++e)
+            if (at + e < n) p[at + e] = v[e];
+    }
 }
-// To the nearest bf16, or up with the probability of the value's place between two of them.
-__device__ __forceinline__ uint32_t to_bf16(float v, uint32_t word, bool dither) {
-    if (dither && (__float_as_uint(v) & 0x7F800000u) != 0x7F800000u) return (__float_as_uint(v) + ((word * 0x9E3779B1u) >> 16)) >> 16;
-    uint16_t r;
-    asm("cvt.rn.bf16.f32 %0, %1;" : "=h"(r) : "f"(v));
+__device__ __forceinline__ uint32_t nearest_bf16x2(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
-__device__ __forceinline__ void store4(uint16_t* p, int64_t at, int left, bool vec, const float (&v)[4], const uint32_t (&word)[4], bool dither) {
-    uint32_t b[4];
+template <bool FULL>
+__device__ __forceinline__ void store4_bf16(uint16_t* p, int64_t at, int64_t n, uint32_t lo, uint32_t hi) {
+    if constexpr (FULL) {
+        *reinterpret_cast<uint2*>(p + at) = make_uint2(lo, hi);
+    } else {
+        const uint32_t b[4] = {lo & 0xFFFFu, lo >> 16, hi & 0xFFFFu, hi >> 16};
 #pragma unroll
-    for (int e = 0; e < 4; ++e) b[e] = to_bf16(v[e], word[e], dither);
-    if (vec && left >= 4) {
-        *reinterpret_cast<uint2*>(p + at) = make_uint2(b[0] | (b[1] << 16), b[2] | (b[3] << 16));
-        return;
+        for (int e = 0; e < 4; ++e)
+            if (at + e < n) p[at + e] = (uint16_t)b[e];
     }
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-        if (e < left) p[at + e] = (uint16_t)b[e];
 }
+// Up to the next bf16 with the probability of the value's place between two of them: a 16-bit random fraction is added to the half that goes.  An
+// infinity stays one; a NaN could carry into the sign and is kept by the caller.
+__device__ __forceinline__ uint32_t dithered(float v, uint32_t word) { return __float_as_uint(v) + ((word * 0x9E3779B1u) >> 16); }
 
 __device__ __forceinline__ float2 decode_pair(uint32_t codes16) {
     const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)codes16, __NV_E4M3);
     return __half22float2(__half2(h));
 }
-__device__ __forceinline__ void decode4(uint32_t codes, float scale, float (&v)[4]) {
+__device__ __forceinline__ void decode4(uint32_t codes, float (&v)[4]) {
     const float2 a = decode_pair(codes & 0xFFFFu), b = decode_pair(codes >> 16);
-    v[0] = a.x * scale; v[1] = a.y * scale; v[2] = b.x * scale; v[3] = b.y * scale;
+    v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
 }
-// A magnitude of up to 448 to one of the two codes around it: the random fraction is added below the three mantissa bits that stay.
-// Under 2^-6 the codes are 2^-9 apart; there the sum is formed in the binade from 2^-6 on, whose codes have that spacing.
-__device__ __forceinline__ float round_to_code(float a, uint32_t bits16) {
-    const float low = a < 0x1p-6f ? 0x1p-6f : 0.f;
-    const float t = __uint_as_float((__float_as_uint(a + low) + (bits16 << 4)) & 0xFFF00000u) - low;
-    return fminf(t, 448.f);
+// A value of up to 448 to one of the two codes around it, in the top byte and without its sign.  Times 2^-120 the 8-bit floats' normal numbers
+// are fp32's (exponent field 1 to 15) and their subnormals fp32's subnormals, so that the code is seven bits of the fp32 pattern; the 20 bits
+// below them are the place between two codes, to which the random fraction is added.
+// (The product in assembly: as C++, nvcc 12.9 pairs it with its neighbour's and returns zeros.)
+__device__ __forceinline__ uint32_t code_of(float y, uint32_t bits16_in_the_middle) {
+    float z;
+    asm("mul.rn.f32 %0, %1, %2;" : "=f"(z) : "f"(y), "f"(0x1p-120f));
+    return min((__float_as_uint(z) << 4) + bits16_in_the_middle, 0x7EFFFFFFu);
 }
-__device__ __forceinline__ uint32_t encode4(const float (&t)[4]) {     // values that are codes already
-    return (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(t[0], t[1]), __NV_SATFINITE, __NV_E4M3) |
-           ((uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(t[2], t[3]), __NV_SATFINITE, __NV_E4M3) << 16);
+__device__ __forceinline__ uint32_t top_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    return __byte_perm(__byte_perm(a, b, 0x0073), __byte_perm(c, d, 0x0073), 0x5410);
 }
-// Largest magnitude of the warp's values as bits (NaN patterns are above infinity), and from it the scale and its reciprocal.  Magnitudes
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+// Largest magnitude of the warp's values (NaN if there is one), and from it the scale and its reciprocal.  Magnitudes
 // below 1e-30 count as zero; a block with an infinity or a NaN gets the scale NaN and stays so.
-__device__ __forceinline__ float block_scale(uint32_t top, float& inverse) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(kFullMask, top, o));
-    const float amax = __uint_as_float(top);
-    if (top >= 0x7F800000u) {
+__device__ __forceinline__ float block_scale(float top, float& inverse) {
+    uint32_t bits = __float_as_uint(top) & 0x7FFFFFFFu;
+    bits = __reduce_max_sync(kFullMask, bits);
+    const float amax = __uint_as_float(bits);
+    if (bits >= 0x7F800000u) {
         inverse = 0.f;
         return __uint_as_float(0x7FC00000u);
     }
@@ -151,10 +160,137 @@ __device__ __forceinline__ float block_scale(uint32_t top, float& inverse) {
     return scale;
 }
 
+// FTZ: values below 2^-126 have the root 0.
+template <bool FTZ>
 __device__ __forceinline__ float approx_sqrt(float x) {
     float r;
-    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+    if (FTZ) asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    else asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
+}
+__device__ __forceinline__ float approx_rcp(float x) {       // x is no subnormal: at least the root of the smallest v, 2^-75
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+// What holds for a tensor.
+struct Step {
+    float beta1, beta2, gain1, gain2;       // gain: (1 - beta) times the gradients' factor, squared for the second moment
+    float eps, decay, rate, root_correction;
+    uint32_t key;
+};
+
+template <typename P, typename G, bool BITS8, bool FULL>
+__device__ __forceinline__ void step_block(const Args& a, const Entry& e, const Step& k, uint32_t inside, int lane) {
+    const size_t arena = (size_t)e.first_block + inside;
+    P* p = reinterpret_cast<P*>(e.p);
+    const G* g = reinterpret_cast<const G*>(e.g);
+    const int64_t at = (int64_t)inside * kBlock + lane * 4;
+    float* master = sizeof(P) == 2 && a.master ? a.master + arena * kBlock : nullptr;
+    float gv[2][4], pv[2][4], mv[2][4], vv[2][4];
+    float m_scale = 1.f, v_scale = 1.f;
+    if constexpr (BITS8) {
+        m_scale = a.m_scale[arena];
+        v_scale = a.v_scale[arena];
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        load4<FULL>(g, at + h * 128, e.n, gv[h]);
+        if (master) load4<true>(master, h * 128 + lane * 4, kBlock, pv[h]);
+        else load4<FULL>(p, at + h * 128, e.n, pv[h]);
+        const size_t quad = arena * (kBlock / 4) + h * 32 + lane;
+        if constexpr (BITS8) {
+            decode4(reinterpret_cast<const uint32_t*>(a.m)[quad], mv[h]);
+            decode4(reinterpret_cast<const uint32_t*>(a.v)[quad], vv[h]);
+        } else {
+            load4<true>(reinterpret_cast<const float*>(a.m), (int64_t)quad * 4, 0, mv[h]);
+            load4<true>(reinterpret_cast<const float*>(a.v), (int64_t)quad * 4, 0, vv[h]);
+        }
+    }
+    float top_m = 0.f, top_v = 0.f;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float gr = gv[h][i];
+            const float root0 = vv[h][i] * v_scale;
+            const float m = fmaf(k.gain1, gr, k.beta1 * (BITS8 ? mv[h][i] * m_scale : mv[h][i]));
+            const float v = fmaf(k.gain2, gr * gr, k.beta2 * (BITS8 ? root0 * root0 : vv[h][i]));
+            const float root = approx_sqrt<BITS8>(v);
+            pv[h][i] = fmaf(pv[h][i], k.decay, -k.rate * (m * approx_rcp(fmaf(root, k.root_correction, k.eps))));
+            mv[h][i] = m;
+            vv[h][i] = BITS8 ? root : v;
+            if (BITS8) {
+                top_m = max_nan(top_m, fabsf(m));
+                top_v = max_nan(top_v, root);
+            }
+        }
+    }
+    float inv_m = 0.f, inv_v = 0.f;
+    if constexpr (BITS8) {
+        m_scale = block_scale(top_m, inv_m);
+        v_scale = block_scale(top_v, inv_v);
+        if (lane == 0) {
+            a.m_scale[arena] = m_scale;
+            a.v_scale[arena] = v_scale;
+        }
+    }
+    const bool dither = sizeof(P) == 2 && a.dither;
+    // The word of place i is mix(i ^ key); the high halves of the eight i are the same, and so is what the first shift brings down.
+    const uint32_t start = ((uint32_t)at ^ k.key) ^ (((uint32_t)at ^ k.key) >> 16);
+    float sum = 0.f;
+    if (dither) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum += pv[h][i];
+    }
+    const bool finite = (__float_as_uint(sum) & 0x7F800000u) != 0x7F800000u;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        uint32_t word[4];
+        if (BITS8 || dither) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) word[i] = mix_rest(start ^ (uint32_t)(h * 128 + i));
+        }
+        if (master) store4<true>(master, h * 128 + lane * 4, kBlock, pv[h]);
+        if constexpr (sizeof(P) == 2) {
+            uint32_t lo, hi;
+            if (dither) {
+                uint32_t b[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    b[i] = dithered(pv[h][i], word[i]);
+                    if (!finite && !isfinite(pv[h][i])) b[i] = __float_as_uint(pv[h][i]);
+                }
+                lo = __byte_perm(b[0], b[1], 0x7632);
+                hi = __byte_perm(b[2], b[3], 0x7632);
+            } else {
+                lo = nearest_bf16x2(pv[h][0], pv[h][1]);
+                hi = nearest_bf16x2(pv[h][2], pv[h][3]);
+            }
+            store4_bf16<FULL>(p, at + h * 128, e.n, lo, hi);
+        } else {
+            store4<FULL>(p, at + h * 128, e.n, pv[h]);
+        }
+        const size_t quad = arena * (kBlock / 4) + h * 32 + lane;
+        if constexpr (BITS8) {
+            uint32_t tm[4], tv[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                tm[i] = code_of(mv[h][i] * inv_m, __byte_perm(word[i], 0, 0x4324));      // the high half, one byte up
+                tv[i] = code_of(vv[h][i] * inv_v, __byte_perm(word[i], 0, 0x4104));      // the low half
+                if (vv[h][i] > 0.f) tv[i] = max(tv[i], 0x01000000u);
+            }
+            const uint32_t signs = top_bytes(__float_as_uint(mv[h][0]), __float_as_uint(mv[h][1]), __float_as_uint(mv[h][2]), __float_as_uint(mv[h][3]));
+            reinterpret_cast<uint32_t*>(a.m)[quad] = (top_bytes(tm[0], tm[1], tm[2], tm[3]) & 0x7F7F7F7Fu) | (signs & 0x80808080u);
+            reinterpret_cast<uint32_t*>(a.v)[quad] = top_bytes(tv[0], tv[1], tv[2], tv[3]) & 0x7F7F7F7Fu;
+        } else {
+            store4<true>(reinterpret_cast<float*>(a.m), (int64_t)quad * 4, 0, mv[h]);
+            store4<true>(reinterpret_cast<float*>(a.v), (int64_t)quad * 4, 0, vv[h]);
+        }
+    }
 }
 
 template <typename P, typename G, bool BITS8>
@@ -162,10 +298,14 @@ __global__ void __launch_bounds__(kThreads)
 adamw_kernel(const __grid_constant__ Args a) {
     const int lane = threadIdx.x & 31;
     const uint32_t warps = gridDim.x * (kThreads / 32);
+    Step k;
     const float grad_factor = a.grad_factor ? *a.grad_factor : 1.f;
+    k.beta1 = a.beta1;
+    k.beta2 = a.beta2;
+    k.gain1 = a.one_minus_beta1 * grad_factor;
+    k.gain2 = a.one_minus_beta2 * grad_factor * grad_factor;
+    k.eps = a.eps;
     uint32_t entry = 0, entry_first = 0, entry_end = 0;
-    float decay = 0.f, rate = 0.f, root_correction = 0.f;
-    uint32_t key = 0;
     for (uint32_t block = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); block < a.blocks; block += warps) {
         if (block >= entry_end) {           // the tensor that this block is part of
             uint32_t lo = entry, hi = a.count;
@@ -180,84 +320,15 @@ adamw_kernel(const __grid_constant__ Args a) {
             const float t = (float)step;
             float lr = a.entry[lo].lr;
             if (a.entry[lo].lr_device) lr = *a.entry[lo].lr_device;
-            decay = 1.f - lr * a.entry[lo].weight_decay;
-            rate = lr / -expm1f(t * a.ln_beta1);
-            root_correction = rsqrtf(-expm1f(t * a.ln_beta2));
-            key = mix(mix(a.seed + step) + a.entry[lo].ordinal);
+            k.decay = 1.f - lr * a.entry[lo].weight_decay;
+            k.rate = lr / -expm1f(t * a.ln_beta1);
+            k.root_correction = rsqrtf(-expm1f(t * a.ln_beta2));
+            k.key = mix(mix(a.seed + step) + a.entry[lo].ordinal);
         }
         const Entry& e = a.entry[entry];
         const uint32_t inside = block - entry_first;
-        const size_t arena = (size_t)e.first_block + inside;
-        P* p = reinterpret_cast<P*>(e.p);
-        const G* g = reinterpret_cast<const G*>(e.g);
-        float gv[2][4], pv[2][4], mv[2][4], vv[2][4];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int64_t at = (int64_t)inside * kBlock + h * 128 + lane * 4;
-            const int left = (int)min((int64_t)4, max((int64_t)0, (int64_t)e.n - at));
-            load4(g, at, left, e.vectors != 0, gv[h]);
-            if (a.master) load4(a.master + arena * kBlock, h * 128 + lane * 4, 4, true, pv[h]);
-            else load4(p, at, left, e.vectors != 0, pv[h]);
-            const size_t quad = arena * (kBlock / 4) + h * 32 + lane;
-            if constexpr (BITS8) {
-                decode4(reinterpret_cast<const uint32_t*>(a.m)[quad], a.m_scale[arena], mv[h]);
-                decode4(reinterpret_cast<const uint32_t*>(a.v)[quad], a.v_scale[arena], vv[h]);
-            } else {
-                load4(reinterpret_cast<const float*>(a.m), (int64_t)quad * 4, 4, true, mv[h]);
-                load4(reinterpret_cast<const float*>(a.v), (int64_t)quad * 4, 4, true, vv[h]);
-            }
-        }
-        uint32_t top_m = 0, top_v = 0, word[2][4] = {};
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float gr = gv[h][i] * grad_factor;
-                const float m = fmaf(a.one_minus_beta1, gr, a.beta1 * mv[h][i]);
-                const float v = fmaf(a.one_minus_beta2, gr * gr, a.beta2 * (BITS8 ? vv[h][i] * vv[h][i] : vv[h][i]));
-                const float root = approx_sqrt(v);
-                pv[h][i] = fmaf(pv[h][i], decay, -rate * __fdividef(m, fmaf(root, root_correction, a.eps)));
-                mv[h][i] = m;
-                vv[h][i] = BITS8 ? root : v;
-                if (BITS8) {
-                    top_m = max(top_m, __float_as_uint(m) & 0x7FFFFFFFu);
-                    top_v = max(top_v, __float_as_uint(root) & 0x7FFFFFFFu);
-                }
-                if (BITS8 || sizeof(P) == 2) word[h][i] = mix((inside * kBlock + h * 128 + lane * 4 + i) ^ key);
-            }
-        }
-        float inv_m = 0.f, inv_v = 0.f, scale_m = 0.f, scale_v = 0.f;
-        if constexpr (BITS8) {
-            scale_m = block_scale(top_m, inv_m);
-            scale_v = block_scale(top_v, inv_v);
-            if (lane == 0) {
-                a.m_scale[arena] = scale_m;
-                a.v_scale[arena] = scale_v;
-            }
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int64_t at = (int64_t)inside * kBlock + h * 128 + lane * 4;
-            const int left = (int)min((int64_t)4, max((int64_t)0, (int64_t)e.n - at));
-            if (a.master) store4(a.master + arena * kBlock, h * 128 + lane * 4, 4, true, pv[h], word[h], false);
-            store4(p, at, left, e.vectors != 0, pv[h], word[h], a.dither != 0);
-            const size_t quad = arena * (kBlock / 4) + h * 32 + lane;
-            if constexpr (BITS8) {
-                float tm[4], tv[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float y = mv[h][i] * inv_m, z = vv[h][i] * inv_v;
-                    tm[i] = copysignf(round_to_code(fabsf(y), word[h][i] >> 16), y);
-                    tv[i] = round_to_code(z, word[h][i] & 0xFFFFu);
-                    if (z > 0.f) tv[i] = fmaxf(tv[i], 0x1p-9f);
-                }
-                reinterpret_cast<uint32_t*>(a.m)[quad] = encode4(tm);
-                reinterpret_cast<uint32_t*>(a.v)[quad] = encode4(tv);
-            } else {
-                store4(reinterpret_cast<float*>(a.m), (int64_t)quad * 4, 4, true, mv[h], word[h], false);
-                store4(reinterpret_cast<float*>(a.v), (int64_t)quad * 4, 4, true, vv[h], word[h], false);
-            }
-        }
+        if (e.vectors && (int64_t)(inside + 1) * kBlock <= (int64_t)e.n) step_block<P, G, BITS8, true>(a, e, k, inside, lane);
+        else step_block<P, G, BITS8, false>(a, e, k, inside, lane);
     }
     // Every CTA has read the step numbers that it needed when it draws its ticket.
     __shared__ uint32_t drawn;

@@ -18,7 +18,7 @@ namespace dropit {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMaxAngles = 2048;            // angles of one block's tokens: 16 KB of shared memory
+constexpr int kMaxAngles = 1024;            // angles of one block's tokens: 8 KB of shared memory
 
 struct RotaryTensor {
     const void* in;
@@ -73,19 +73,26 @@ __device__ __forceinline__ float half_turns(const RotaryArgs& a, int64_t offset,
     return (float)(int32_t)(((uint64_t)p * turns) >> 32) * 0x1p-31f;
 }
 
-// A unit is VP pairs of one head (two vectors of VP values), or VP of the values behind the rotated ones, which are copied.
+// A unit is VP pairs of one head (two vectors of VP values), or VP of the values behind the rotated ones, which are copied.  A thread keeps its
+// place in the head and steps through the rows (token, head) of the block without dividing; two rows' loads are in flight at a time.
 template <typename T, int VP, bool INTERLEAVED>
 __global__ void __launch_bounds__(kThreads)
 rotary_kernel(const __grid_constant__ RotaryArgs a) {
-    __shared__ float2 angles[kMaxAngles];
+    extern __shared__ float2 angles[];                                   // [tokens][pairs], then the tokens' places
     const int pairs = a.plan.pairs;
     const int64_t first = (int64_t)blockIdx.x * a.tokens_per_block;
     const int tokens = (int)min((int64_t)a.tokens_per_block, a.tokens - first);
+    longlong4* places = reinterpret_cast<longlong4*>(angles + (a.tokens_per_block * pairs + 3) / 4 * 4);   // q in, q out, k in, k out
+    for (int i = threadIdx.x; i < tokens; i += kThreads) {
+        const int64_t token = first + i, batch = token / a.length, at = token - batch * a.length;
+        places[i] = make_longlong4(batch * a.t[0].in_batch + at * a.t[0].in_token, batch * a.t[0].out_batch + at * a.t[0].out_token,
+                                   batch * a.t[1].in_batch + at * a.t[1].in_token, batch * a.t[1].out_batch + at * a.t[1].out_token);
+    }
     for (int i = threadIdx.x; i < tokens * pairs; i += kThreads) {
-        const int64_t token = first + i / pairs;
-        const int64_t batch = token / a.length;
+        const int local = i / pairs;
+        const int64_t token = first + local, batch = token / a.length;
         float2 cs;
-        sincospif(half_turns(a, batch * a.pos_batch + (token - batch * a.length) * a.pos_token, i % pairs), &cs.y, &cs.x);
+        sincospif(half_turns(a, batch * a.pos_batch + (token - batch * a.length) * a.pos_token, i - local * pairs), &cs.y, &cs.x);
         cs.y *= a.sign;
         angles[i] = cs;
     }
@@ -93,49 +100,70 @@ rotary_kernel(const __grid_constant__ RotaryArgs a) {
     const int rotating = pairs / VP;
     const int units = rotating + (a.head_dim - 2 * pairs) / VP;
     const int heads = a.t[0].heads + a.t[1].heads;
-    const int total = tokens * heads * units;
-    for (int i = threadIdx.x; i < total; i += kThreads) {
-        const int row = i / units, unit = i - row * units;
-        const int local = row / heads;
-        int head = row - local * heads;
-        const int64_t token = first + local;
-        const int64_t batch = token / a.length, at = token - batch * a.length;
-        const int which = head >= a.t[0].heads;
-        const RotaryTensor& t = a.t[which];
-        if (which) head -= a.t[0].heads;
-        const T* in = reinterpret_cast<const T*>(t.in) + batch * t.in_batch + at * t.in_token + head * t.in_head;
-        T* out = reinterpret_cast<T*>(t.out) + batch * t.out_batch + at * t.out_token + head * t.out_head;
-        using Vec = Values<T, VP>;
-        using B = typename Bits<VP * sizeof(T)>::type;
-        if (unit >= rotating) {
-            const int c = 2 * pairs + (unit - rotating) * VP;
-            *reinterpret_cast<B*>(out + c) = *reinterpret_cast<const B*>(in + c);
-            continue;
-        }
-        const int c0 = INTERLEAVED ? 2 * unit * VP : unit * VP;
+    using Vec = Values<T, VP>;
+    using B = typename Bits<VP * sizeof(T)>::type;
+    for (int unit0 = 0; unit0 < units; unit0 += kThreads) {              // one round, unless a head has more units than the block threads
+        const int width = min(units - unit0, kThreads), step = kThreads / width;
+        const int unit = unit0 + threadIdx.x % width;
+        int head = threadIdx.x / width, local = 0;
+        if (head >= step) continue;
+        const int c0 = unit >= rotating ? 2 * pairs + (unit - rotating) * VP : INTERLEAVED ? 2 * unit * VP : unit * VP;
         const int c1 = INTERLEAVED ? c0 + VP : pairs + c0;
-        Vec x, y;
-        x.bits = *reinterpret_cast<const B*>(in + c0);
-        y.bits = *reinterpret_cast<const B*>(in + c1);
-        const float2* cs = angles + local * pairs + unit * VP;
+        const bool copies = unit >= rotating;
+        while (head >= heads) head -= heads, ++local;
+        while (local < tokens) {
+            const T* in[2];
+            T* out[2];
+            int token[2], live = 0;
 #pragma unroll
-        for (int e = 0; e < VP; ++e) {
-            // halves: pair e is (x[e], y[e]); neighbours: values 2e and 2e + 1 of x followed by y
-            T& one = INTERLEAVED ? (2 * e < VP ? x.v[2 * e % VP] : y.v[2 * e % VP]) : x.v[e];
-            T& two = INTERLEAVED ? (2 * e + 1 < VP ? x.v[(2 * e + 1) % VP] : y.v[(2 * e + 1) % VP]) : y.v[e];
-            const float u = to_float(one), v = to_float(two);
-            from_float(u * cs[e].x - v * cs[e].y, one);
-            from_float(u * cs[e].y + v * cs[e].x, two);
+            for (int r = 0; r < 2; ++r) {
+                token[r] = local;
+                if (local < tokens) {
+                    const longlong4 place = places[local];
+                    const bool key = head >= a.t[0].heads;
+                    const RotaryTensor& t = a.t[key];
+                    const int64_t h = key ? head - a.t[0].heads : head;
+                    in[r] = reinterpret_cast<const T*>(t.in) + (key ? place.z : place.x) + h * t.in_head;
+                    out[r] = reinterpret_cast<T*>(t.out) + (key ? place.w : place.y) + h * t.out_head;
+                    ++live;
+                    head += step;
+                    while (head >= heads) head -= heads, ++local;
+                }
+            }
+            Vec x[2], y[2];
+#pragma unroll
+            for (int r = 0; r < 2; ++r)
+                if (r < live) {
+                    x[r].bits = *reinterpret_cast<const B*>(in[r] + c0);
+                    if (!copies) y[r].bits = *reinterpret_cast<const B*>(in[r] + c1);
+                }
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                if (r >= live) break;
+                if (!copies) {
+                    const float2* cs = angles + token[r] * pairs + unit * VP;
+#pragma unroll
+                    for (int e = 0; e < VP; ++e) {
+                        // halves: pair e is (x[e], y[e]); neighbours: values 2e and 2e + 1 of x followed by y
+                        T& one = INTERLEAVED ? (2 * e < VP ? x[r].v[2 * e % VP] : y[r].v[2 * e % VP]) : x[r].v[e];
+                        T& two = INTERLEAVED ? (2 * e + 1 < VP ? x[r].v[(2 * e + 1) % VP] : y[r].v[(2 * e + 1) % VP]) : y[r].v[e];
+                        const float u = to_float(one), v = to_float(two);
+                        from_float(u * cs[e].x - v * cs[e].y, one);
+                        from_float(u * cs[e].y + v * cs[e].x, two);
+                    }
+                    *reinterpret_cast<B*>(out[r] + c1) = y[r].bits;
+                }
+                *reinterpret_cast<B*>(out[r] + c0) = x[r].bits;
+            }
         }
-        *reinterpret_cast<B*>(out + c0) = x.bits;
-        *reinterpret_cast<B*>(out + c1) = y.bits;
     }
 }
 
 template <typename T, int VP>
 void launch(const RotaryArgs& a, unsigned blocks, cudaStream_t stream) {
-    if (a.plan.interleaved) rotary_kernel<T, VP, true><<<blocks, kThreads, 0, stream>>>(a);
-    else rotary_kernel<T, VP, false><<<blocks, kThreads, 0, stream>>>(a);
+    const size_t smem = (size_t)((a.tokens_per_block * a.plan.pairs + 3) / 4 * 4) * sizeof(float2) + (size_t)a.tokens_per_block * sizeof(longlong4);
+    if (a.plan.interleaved) rotary_kernel<T, VP, true><<<blocks, kThreads, smem, stream>>>(a);
+    else rotary_kernel<T, VP, false><<<blocks, kThreads, smem, stream>>>(a);
 }
 
 // Whether vectors of `n` values of `size` bytes fit everywhere.
@@ -230,7 +258,7 @@ extern "C" dropit_status dropit_rotary(const dropit_rotary_plan* plan, int64_t b
     // Four units a thread, as far as the angles fit and every SM has blocks.
     const int64_t units = heads * ((plan->head_dim - plan->pairs) / vec);
     int64_t per_block = (4 * kThreads + units - 1) / units;
-    per_block = std::min<int64_t>(per_block, kMaxAngles / plan->pairs);
+    per_block = std::min<int64_t>(std::min<int64_t>(per_block, kMaxAngles / plan->pairs), 256);
     per_block = std::min<int64_t>(per_block, std::max<int64_t>(1, tokens / (2 * sm_count())));
     a.tokens_per_block = (int)std::max<int64_t>(1, per_block);
     const int64_t blocks = (tokens + a.tokens_per_block - 1) / a.tokens_per_block;
