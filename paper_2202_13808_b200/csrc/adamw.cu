@@ -16,6 +16,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
@@ -29,24 +30,25 @@ namespace {
 constexpr int kBlock = DROPIT_ADAMW_BLOCK;
 constexpr int kThreads = 256;
 constexpr int kMaxEntries = 512;
+constexpr uint32_t kMaxRun = 8;                     // blocks of a run: a sector of scales
+constexpr int kResident8 = 3, kResident32 = 2;          // CTAs per SM: 8 bits 199 / 187 / 226 us with 2 / 3 / 4 (the last spills), 32 bits 387 / 390 with 2 / 3
 
 struct Entry {
     void* p;
     const void* g;
     const float* lr_device;
     uint32_t first_block;       // in the arenas
-    uint32_t before;            // blocks of this launch's tensors in front of this one
+    uint32_t before;            // runs of this launch's tensors in front of this one
     uint32_t n;
     uint32_t ordinal;
     float lr, weight_decay;
-    uint32_t vectors;           // p and g are aligned for loads of four values
+    uint32_t vectors;           // p and g are aligned to 16 bytes
     uint32_t reserved;
 };
 struct Args {
     float beta1, beta2, one_minus_beta1, one_minus_beta2, ln_beta1, ln_beta2, eps;
     uint32_t seed;              // already mixed
-    uint32_t blocks, count;
-    int dither;
+    uint32_t runs, run, count;      // run: blocks of one
     void* m;
     void* v;
     float* m_scale;
@@ -68,96 +70,128 @@ __host__ __device__ __forceinline__ uint32_t mix_rest(uint32_t x) {       // all
 }
 __host__ __device__ __forceinline__ uint32_t mix(uint32_t x) { return mix_rest(x ^ (x >> 16)); }
 
-// ---- four values of a lane, FULL: all inside the tensor and aligned ----
-template <bool FULL>
-__device__ __forceinline__ void load4(const float* p, int64_t at, int64_t n, float (&v)[4]) {
+// ---- a lane's eight values of a block: neighbours where moments are in 8 bits (16 bytes of bf16, 8 of codes), else two quads of fp32 ----
+template <bool BITS8>
+__device__ __forceinline__ int lane_start(int lane) { return BITS8 ? lane * 8 : lane * 4; }
+template <bool BITS8>
+__host__ __device__ constexpr int place_of(int i) { return BITS8 ? i : (i >> 2) * 128 + (i & 3); }
+
+// The words that eight values of type T are held in, and how they come and go.  at: the lane's first value; left: values from there to the tensor's end.
+template <typename T> constexpr int kWords = sizeof(T) * 2;
+template <typename T, bool BITS8, bool FULL>
+__device__ __forceinline__ void load8(const T* p, int64_t left, uint32_t (&w)[kWords<T>]) {
     if constexpr (FULL) {
-        const float4 q = *reinterpret_cast<const float4*>(p + at);
-        v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
+        if constexpr (sizeof(T) == 4 || !BITS8) {
+            using Quad = typename std::conditional<sizeof(T) == 4, uint4, uint2>::type;
+            const Quad q[2] = {*reinterpret_cast<const Quad*>(p), *reinterpret_cast<const Quad*>(p + place_of<BITS8>(4))};
+            if constexpr (sizeof(T) == 4) {
+                w[0] = q[0].x; w[1] = q[0].y; w[2] = q[0].z; w[3] = q[0].w; w[4] = q[1].x; w[5] = q[1].y; w[6] = q[1].z; w[7] = q[1].w;
+            } else {
+                w[0] = q[0].x; w[1] = q[0].y; w[2] = q[1].x; w[3] = q[1].y;
+            }
+        } else {
+            const uint4 q = *reinterpret_cast<const uint4*>(p);
+            w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
+        }
     } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = at + e < n ? p[at + e] : 0.f;
+        for (int i = 0; i < kWords<T>; ++i) w[i] = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (place_of<BITS8>(i) >= left) continue;
+            if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(p[place_of<BITS8>(i)]);
+            else w[i / 2] |= (uint32_t)p[place_of<BITS8>(i)] << (16 * (i & 1));
+        }
     }
 }
-template <bool FULL>
-__device__ __forceinline__ void load4(const uint16_t* p, int64_t at, int64_t n, float (&v)[4]) {
+template <typename T, bool BITS8, bool FULL>
+__device__ __forceinline__ void store8(T* p, int64_t left, const uint32_t (&w)[kWords<T>]) {
     if constexpr (FULL) {
-        const uint2 q = *reinterpret_cast<const uint2*>(p + at);
-        v[0] = __uint_as_float(q.x << 16); v[1] = __uint_as_float(q.x & 0xFFFF0000u);
-        v[2] = __uint_as_float(q.y << 16); v[3] = __uint_as_float(q.y & 0xFFFF0000u);
+        if constexpr (sizeof(T) == 4) {
+            *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+            *reinterpret_cast<uint4*>(p + place_of<BITS8>(4)) = make_uint4(w[4], w[5], w[6], w[7]);
+        } else if constexpr (!BITS8) {
+            *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+            *reinterpret_cast<uint2*>(p + place_of<BITS8>(4)) = make_uint2(w[2], w[3]);
+        } else {
+            *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
     } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = at + e < n ? __uint_as_float((uint32_t)p[at + e] << 16) : 0.f;
+        for (int i = 0; i < 8; ++i) {
+            if (place_of<BITS8>(i) >= left) continue;
+            if constexpr (sizeof(T) == 4) p[place_of<BITS8>(i)] = __uint_as_float(w[i]);
+            else p[place_of<BITS8>(i)] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+        }
     }
 }
-template <bool FULL>
-__device__ __forceinline__ void store4(float* p, int64_t at, int64_t n, const float (&v)[4]) {
-    if constexpr (FULL) {
-        *reinterpret_cast<float4*>(p + at) = make_float4(v[0], v[1], v[2], v[3]);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (at + e < n) p[at + e] = v[e];
-    }
+template <int WORDS>
+__device__ __forceinline__ float value_of(const uint32_t (&w)[WORDS], int i) {
+    if constexpr (WORDS == 8) return __uint_as_float(w[i]);
+    else return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
 }
 __device__ __forceinline__ uint32_t nearest_bf16x2(float lo, float hi) {
     uint32_t r;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
-template <bool FULL>
-__device__ __forceinline__ void store4_bf16(uint16_t* p, int64_t at, int64_t n, uint32_t lo, uint32_t hi) {
-    if constexpr (FULL) {
-        *reinterpret_cast<uint2*>(p + at) = make_uint2(lo, hi);
-    } else {
-        const uint32_t b[4] = {lo & 0xFFFFu, lo >> 16, hi & 0xFFFFu, hi >> 16};
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (at + e < n) p[at + e] = (uint16_t)b[e];
-    }
-}
 // Up to the next bf16 with the probability of the value's place between two of them: a 16-bit random fraction is added to the half that goes.  An
 // infinity stays one; a NaN could carry into the sign and is kept by the caller.
 __device__ __forceinline__ uint32_t dithered(float v, uint32_t word) { return __float_as_uint(v) + ((word * 0x9E3779B1u) >> 16); }
 
+// Products in assembly: nvcc 12.9 otherwise pairs them into 64-bit registers, which costs more moves than it saves products (and for products with
+// 2^-120 it returned zeros).
+__device__ __forceinline__ float mul(float a, float b) {
+    float r;
+    asm("mul.rn.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float fma(float a, float b, float c) {
+    float r;
+    asm("fma.rn.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+
+// Two 8-bit floats.
 __device__ __forceinline__ float2 decode_pair(uint32_t codes16) {
     const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)codes16, __NV_E4M3);
     return __half22float2(__half2(h));
 }
-__device__ __forceinline__ void decode4(uint32_t codes, float (&v)[4]) {
-    const float2 a = decode_pair(codes & 0xFFFFu), b = decode_pair(codes >> 16);
-    v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
-}
-// A value of up to 448 to one of the two codes around it, in the top byte and without its sign.  Times 2^-120 the 8-bit floats' normal numbers
-// are fp32's (exponent field 1 to 15) and their subnormals fp32's subnormals, so that the code is seven bits of the fp32 pattern; the 20 bits
-// below them are the place between two codes, to which the random fraction is added.
-// (The product in assembly: as C++, nvcc 12.9 pairs it with its neighbour's and returns zeros.)
-__device__ __forceinline__ uint32_t code_of(float y, uint32_t bits16_in_the_middle) {
-    float z;
-    asm("mul.rn.f32 %0, %1, %2;" : "=f"(z) : "f"(y), "f"(0x1p-120f));
-    return min((__float_as_uint(z) << 4) + bits16_in_the_middle, 0x7EFFFFFFu);
-}
+// A value of less than 448 to one of the two codes around it, in the top byte and without its sign; z is the pattern of 2^-120 times the value.  There
+// the 8-bit floats' normal numbers are fp32's (exponent field 1 to 15) and their subnormals fp32's subnormals, so that the code is seven bits
+// of the pattern; the 20 bits below them are the place between two codes, to which the random fraction is added.
+__device__ __forceinline__ uint32_t code_of(uint32_t z, uint32_t bits16_in_the_middle) { return (z << 4) + bits16_in_the_middle; }
 __device__ __forceinline__ uint32_t top_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     return __byte_perm(__byte_perm(a, b, 0x0073), __byte_perm(c, d, 0x0073), 0x5410);
 }
-__device__ __forceinline__ float max_nan(float a, float b) {
+__device__ __forceinline__ float max_nan(float a, float b, float c) {
     float r;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
-// Largest magnitude of the warp's values (NaN if there is one), and from it the scale and its reciprocal.  Magnitudes
-// below 1e-30 count as zero; a block with an infinity or a NaN gets the scale NaN and stays so.
-__device__ __forceinline__ float block_scale(float top, float& inverse) {
+__device__ __forceinline__ float approx_rcp(float x) {       // neither x nor 1 / x is subnormal
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+// Largest magnitude of the warp's values (NaN if there is one), and from it the scale.  Magnitudes below 1e-30 count as zero; a block with an infinity
+// or a NaN gets the scale NaN and stays so.  `factor` takes the values to 2^-120 of their share of 448: the scale's reciprocal, 2^-20 of itself short,
+// which keeps every share below 448 whatever the roundings, times 2^-120.  Where that product would be subnormal (magnitudes above
+// 2^14), the values take the reciprocal first.
+__device__ __forceinline__ float block_scale(float top, float (&values)[8], float& factor) {
     uint32_t bits = __float_as_uint(top) & 0x7FFFFFFFu;
     bits = __reduce_max_sync(kFullMask, bits);
-    const float amax = __uint_as_float(bits);
-    if (bits >= 0x7F800000u) {
-        inverse = 0.f;
-        return __uint_as_float(0x7FC00000u);
+    const float amax = __uint_as_float(bits), scale = mul(amax, 1.f / 448.f);
+    if (bits - 0x0DA24260u < 0x46800000u - 0x0DA24260u) {           // 1e-30 <= amax < 2^14
+        factor = mul(mul(approx_rcp(scale), 1.f - 0x1p-20f), 0x1p-120f);
+        return scale;
     }
-    const float scale = amax < 1e-30f ? 0.f : __fdiv_rn(amax, 448.f);
-    inverse = scale > 0.f ? __frcp_rn(scale) : 0.f;
-    return scale;
+    const bool none = amax < 1e-30f, bad = bits >= 0x7F800000u;
+    const float inverse = none || bad ? 0.f : mul(approx_rcp(scale), 1.f - 0x1p-20f);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) values[i] = mul(values[i], inverse);
+    factor = 0x1p-120f;
+    return bad ? __uint_as_float(0x7FC00000u) : none ? 0.f : scale;
 }
 
 // FTZ: values below 2^-126 have the root 0.
@@ -168,154 +202,195 @@ __device__ __forceinline__ float approx_sqrt(float x) {
     else asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
-__device__ __forceinline__ float approx_rcp(float x) {       // x is no subnormal: at least the root of the smallest v, 2^-75
-    float r;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-    return r;
-}
-
 // What holds for a tensor.
 struct Step {
     float beta1, beta2, gain1, gain2;       // gain: (1 - beta) times the gradients' factor, squared for the second moment
+    float root_beta2, root_gain2;           // their roots: moments in 8 bits hold sqrt(v)
     float eps, decay, rate, root_correction;
     uint32_t key;
+    void* p;
+    const void* g;
+    uint32_t first_block, n, whole;         // whole: its first blocks, all inside and aligned
 };
 
-template <typename P, typename G, bool BITS8, bool FULL>
-__device__ __forceinline__ void step_block(const Args& a, const Entry& e, const Step& k, uint32_t inside, int lane) {
-    const size_t arena = (size_t)e.first_block + inside;
-    P* p = reinterpret_cast<P*>(e.p);
-    const G* g = reinterpret_cast<const G*>(e.g);
-    const int64_t at = (int64_t)inside * kBlock + lane * 4;
-    float* master = sizeof(P) == 2 && a.master ? a.master + arena * kBlock : nullptr;
-    float gv[2][4], pv[2][4], mv[2][4], vv[2][4];
-    float m_scale = 1.f, v_scale = 1.f;
+// How a bf16 parameter is stepped: rounded to nearest, rounded with a dither, or in an fp32 copy of it (then either).
+enum { kNearest = 0, kDither = 1, kMaster = 2, kMasterDither = 3 };
+
+// A lane's share of a block as it lies in memory.
+template <typename P, typename G, bool BITS8, int FORM>
+struct Raw {
+    uint32_t p[(FORM & kMaster) ? 8 : kWords<P>], g[kWords<G>], m[BITS8 ? 2 : 8], v[BITS8 ? 2 : 8];
+    float m_scale, r_scale;
+};
+
+template <typename P, typename G, bool BITS8, int FORM, bool FULL>
+__device__ __forceinline__ void load_block(const Args& a, const Step& k, uint32_t inside, int lane, Raw<P, G, BITS8, FORM>& raw) {
+    const size_t arena = (size_t)k.first_block + inside;
+    const uint32_t at = inside * kBlock + lane_start<BITS8>(lane);
+    const int64_t left = (int64_t)k.n - at;
+    load8<G, BITS8, FULL>(reinterpret_cast<const G*>(k.g) + at, left, raw.g);
+    if constexpr ((FORM & kMaster) != 0) load8<float, BITS8, true>(a.master + arena * kBlock + lane_start<BITS8>(lane), 0, raw.p);
+    else load8<P, BITS8, FULL>(reinterpret_cast<const P*>(k.p) + at, left, raw.p);
     if constexpr (BITS8) {
-        m_scale = a.m_scale[arena];
-        v_scale = a.v_scale[arena];
+        const uint2 m = reinterpret_cast<const uint2*>(a.m)[arena * 32 + lane], v = reinterpret_cast<const uint2*>(a.v)[arena * 32 + lane];
+        raw.m[0] = m.x; raw.m[1] = m.y; raw.v[0] = v.x; raw.v[1] = v.y;
+    } else {
+        load8<float, false, true>(reinterpret_cast<const float*>(a.m) + arena * kBlock + lane_start<false>(lane), 0, raw.m);
+        load8<float, false, true>(reinterpret_cast<const float*>(a.v) + arena * kBlock + lane_start<false>(lane), 0, raw.v);
     }
+}
+
+// A lane's share of a block after the step: p, m, and v or its root.
+struct Stepped {
+    float p[8], m[8], v[8];
+    float top_m, top_r;         // largest magnitudes
+};
+
+template <typename P, typename G, bool BITS8, int FORM>
+__device__ __forceinline__ void compute(const Step& k, const Raw<P, G, BITS8, FORM>& raw, Stepped& s) {
+    const float m_factor = BITS8 ? k.beta1 * raw.m_scale : k.beta1, v_factor = BITS8 ? k.root_beta2 * raw.r_scale : k.beta2;
+    s.top_m = s.top_r = 0.f;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        load4<FULL>(g, at + h * 128, e.n, gv[h]);
-        if (master) load4<true>(master, h * 128 + lane * 4, kBlock, pv[h]);
-        else load4<FULL>(p, at + h * 128, e.n, pv[h]);
-        const size_t quad = arena * (kBlock / 4) + h * 32 + lane;
+    for (int i = 0; i < 8; i += 2) {
+        float m0[2], v0[2];
         if constexpr (BITS8) {
-            decode4(reinterpret_cast<const uint32_t*>(a.m)[quad], mv[h]);
-            decode4(reinterpret_cast<const uint32_t*>(a.v)[quad], vv[h]);
+            const int shift = 16 * ((i >> 1) & 1);
+            const float2 m = decode_pair((raw.m[i / 4] >> shift) & 0xFFFFu), r = decode_pair((raw.v[i / 4] >> shift) & 0xFFFFu);
+            m0[0] = m.x, m0[1] = m.y, v0[0] = r.x, v0[1] = r.y;
         } else {
-            load4<true>(reinterpret_cast<const float*>(a.m), (int64_t)quad * 4, 0, mv[h]);
-            load4<true>(reinterpret_cast<const float*>(a.v), (int64_t)quad * 4, 0, vv[h]);
+            m0[0] = __uint_as_float(raw.m[i]), m0[1] = __uint_as_float(raw.m[i + 1]);
+            v0[0] = __uint_as_float(raw.v[i]), v0[1] = __uint_as_float(raw.v[i + 1]);
         }
-    }
-    float top_m = 0.f, top_v = 0.f;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float gr = gv[h][i];
-            const float root0 = vv[h][i] * v_scale;
-            const float m = fmaf(k.gain1, gr, k.beta1 * (BITS8 ? mv[h][i] * m_scale : mv[h][i]));
-            const float v = fmaf(k.gain2, gr * gr, k.beta2 * (BITS8 ? root0 * root0 : vv[h][i]));
-            const float root = approx_sqrt<BITS8>(v);
-            pv[h][i] = fmaf(pv[h][i], k.decay, -k.rate * (m * approx_rcp(fmaf(root, k.root_correction, k.eps))));
-            mv[h][i] = m;
-            vv[h][i] = BITS8 ? root : v;
-            if (BITS8) {
-                top_m = max_nan(top_m, fabsf(m));
-                top_v = max_nan(top_v, root);
-            }
-        }
-    }
-    float inv_m = 0.f, inv_v = 0.f;
-    if constexpr (BITS8) {
-        m_scale = block_scale(top_m, inv_m);
-        v_scale = block_scale(top_v, inv_v);
-        if (lane == 0) {
-            a.m_scale[arena] = m_scale;
-            a.v_scale[arena] = v_scale;
-        }
-    }
-    const bool dither = sizeof(P) == 2 && a.dither;
-    // The word of place i is mix(i ^ key); the high halves of the eight i are the same, and so is what the first shift brings down.
-    const uint32_t start = ((uint32_t)at ^ k.key) ^ (((uint32_t)at ^ k.key) >> 16);
-    float sum = 0.f;
-    if (dither) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sum += pv[h][i];
-    }
-    const bool finite = (__float_as_uint(sum) & 0x7F800000u) != 0x7F800000u;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        uint32_t word[4];
-        if (BITS8 || dither) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) word[i] = mix_rest(start ^ (uint32_t)(h * 128 + i));
-        }
-        if (master) store4<true>(master, h * 128 + lane * 4, kBlock, pv[h]);
-        if constexpr (sizeof(P) == 2) {
-            uint32_t lo, hi;
-            if (dither) {
-                uint32_t b[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    b[i] = dithered(pv[h][i], word[i]);
-                    if (!finite && !isfinite(pv[h][i])) b[i] = __float_as_uint(pv[h][i]);
-                }
-                lo = __byte_perm(b[0], b[1], 0x7632);
-                hi = __byte_perm(b[2], b[3], 0x7632);
+        for (int e = 0; e < 2; ++e) {
+            const float g = value_of(raw.g, i + e);
+            const float m = fma(k.gain1, g, mul(m0[e], m_factor));
+            float v;
+            if constexpr (BITS8) {
+                const float r = mul(v0[e], v_factor), q = mul(g, k.root_gain2);
+                v = fma(r, r, mul(q, q));
             } else {
-                lo = nearest_bf16x2(pv[h][0], pv[h][1]);
-                hi = nearest_bf16x2(pv[h][2], pv[h][3]);
+                v = fma(k.gain2, mul(g, g), mul(v0[e], v_factor));
             }
-            store4_bf16<FULL>(p, at + h * 128, e.n, lo, hi);
-        } else {
-            store4<FULL>(p, at + h * 128, e.n, pv[h]);
+            const float root = approx_sqrt<BITS8>(v);
+            const float move = mul(m, approx_rcp(fma(root, k.root_correction, k.eps)));
+            s.p[i + e] = fma(value_of(raw.p, i + e), k.decay, mul(-k.rate, move));
+            s.m[i + e] = m;
+            s.v[i + e] = BITS8 ? root : v;
         }
-        const size_t quad = arena * (kBlock / 4) + h * 32 + lane;
         if constexpr (BITS8) {
-            uint32_t tm[4], tv[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                tm[i] = code_of(mv[h][i] * inv_m, __byte_perm(word[i], 0, 0x4324));      // the high half, one byte up
-                tv[i] = code_of(vv[h][i] * inv_v, __byte_perm(word[i], 0, 0x4104));      // the low half
-                if (vv[h][i] > 0.f) tv[i] = max(tv[i], 0x01000000u);
-            }
-            const uint32_t signs = top_bytes(__float_as_uint(mv[h][0]), __float_as_uint(mv[h][1]), __float_as_uint(mv[h][2]), __float_as_uint(mv[h][3]));
-            reinterpret_cast<uint32_t*>(a.m)[quad] = (top_bytes(tm[0], tm[1], tm[2], tm[3]) & 0x7F7F7F7Fu) | (signs & 0x80808080u);
-            reinterpret_cast<uint32_t*>(a.v)[quad] = top_bytes(tv[0], tv[1], tv[2], tv[3]) & 0x7F7F7F7Fu;
-        } else {
-            store4<true>(reinterpret_cast<float*>(a.m), (int64_t)quad * 4, 0, mv[h]);
-            store4<true>(reinterpret_cast<float*>(a.v), (int64_t)quad * 4, 0, vv[h]);
+            s.top_m = max_nan(s.top_m, fabsf(s.m[i]), fabsf(s.m[i + 1]));
+            s.top_r = max_nan(s.top_r, s.v[i], s.v[i + 1]);
         }
     }
 }
 
-template <typename P, typename G, bool BITS8>
-__global__ void __launch_bounds__(kThreads)
+template <typename P, typename G, bool BITS8, int FORM, bool FULL>
+__device__ __forceinline__ void write(const Args& a, const Step& k, uint32_t inside, int lane, Stepped& s, float& m_scale, float& r_scale) {
+    constexpr bool kCopy = (FORM & kMaster) != 0, kDithers = (FORM & kDither) != 0;
+    const size_t arena = (size_t)k.first_block + inside;
+    const uint32_t at = inside * kBlock + lane_start<BITS8>(lane);
+    const int64_t left = (int64_t)k.n - at;
+    // The word of place i is mix(i ^ key); the high halves of a lane's eight i are the same, and so is what the first shift brings down.
+    uint32_t word[8];
+    if constexpr (BITS8 || kDithers) {
+        const uint32_t start = (at ^ k.key) ^ ((at ^ k.key) >> 16);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) word[i] = mix_rest(start ^ (uint32_t)place_of<BITS8>(i));
+    }
+    if constexpr (kCopy) {
+        uint32_t w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(s.p[i]);
+        store8<float, BITS8, true>(a.master + arena * kBlock + lane_start<BITS8>(lane), 0, w);
+    }
+    if constexpr (sizeof(P) == 2) {
+        uint32_t w[4];
+        if constexpr (kDithers) {
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) w[i / 2] = __byte_perm(dithered(s.p[i], word[i]), dithered(s.p[i + 1], word[i + 1]), 0x7632);
+            const float sum = ((s.p[0] + s.p[1]) + (s.p[2] + s.p[3])) + ((s.p[4] + s.p[5]) + (s.p[6] + s.p[7]));
+            if (!isfinite(sum)) {
+#pragma unroll
+                for (int i = 0; i < 8; i += 2) {
+                    const uint32_t lo = isfinite(s.p[i]) ? w[i / 2] & 0xFFFFu : __float_as_uint(s.p[i]) >> 16;
+                    const uint32_t hi = isfinite(s.p[i + 1]) ? w[i / 2] >> 16 : __float_as_uint(s.p[i + 1]) >> 16;
+                    w[i / 2] = lo | (hi << 16);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) w[i / 2] = nearest_bf16x2(s.p[i], s.p[i + 1]);
+        }
+        store8<P, BITS8, FULL>(reinterpret_cast<P*>(k.p) + at, left, w);
+    } else {
+        uint32_t w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(s.p[i]);
+        store8<P, BITS8, FULL>(reinterpret_cast<P*>(k.p) + at, left, w);
+    }
+    if constexpr (BITS8) {
+        float for_m, for_r;
+        m_scale = block_scale(s.top_m, s.m, for_m);
+        r_scale = block_scale(s.top_r, s.v, for_r);
+        uint32_t m[2], r[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            uint32_t tm[4], tr[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t zm = __float_as_uint(mul(s.m[4 * h + i], for_m));
+                tm[i] = (code_of(zm, __byte_perm(word[4 * h + i], 0, 0x4324)) & 0x7FFFFFFFu) | (zm & 0x80000000u);      // the high half, one byte up
+                tr[i] = code_of(__float_as_uint(mul(s.v[4 * h + i], for_r)), __byte_perm(word[4 * h + i], 0, 0x4104));   // the low half
+            }
+            m[h] = top_bytes(tm[0], tm[1], tm[2], tm[3]);
+            r[h] = top_bytes(tr[0], tr[1], tr[2], tr[3]);
+            if ((r[h] - 0x01010101u) & ~r[h] & 0x80808080u) {         // a code is zero: the smallest one where the root is not
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (s.v[4 * h + i] > 0.f && !(r[h] >> (8 * i) & 0xFFu)) r[h] |= 1u << (8 * i);
+            }
+        }
+        reinterpret_cast<uint2*>(a.m)[arena * 32 + lane] = make_uint2(m[0], m[1]);
+        reinterpret_cast<uint2*>(a.v)[arena * 32 + lane] = make_uint2(r[0], r[1]);
+    } else {
+        uint32_t m[8], v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m[i] = __float_as_uint(s.m[i]), v[i] = __float_as_uint(s.v[i]);
+        store8<float, false, true>(reinterpret_cast<float*>(a.m) + arena * kBlock + lane_start<false>(lane), 0, m);
+        store8<float, false, true>(reinterpret_cast<float*>(a.v) + arena * kBlock + lane_start<false>(lane), 0, v);
+    }
+}
+
+// Warps take runs of a tensor's blocks in turn (a.run of them, fewer where that leaves warps without any), so that the tensor's constants are
+// looked up and the scales of a run come and go once; the next block's loads are under way while one is rounded and written.
+// 85 M bf16 values with moments in 8 bits: 187 us; 268 with single blocks dealt out (nearly every one another tensor's), 295 with one stretch of
+// blocks a CTA, whose streams keep in step.
+template <typename P, typename G, bool BITS8, int FORM>
+__global__ void __launch_bounds__(kThreads, BITS8 ? kResident8 : kResident32)
 adamw_kernel(const __grid_constant__ Args a) {
     const int lane = threadIdx.x & 31;
-    const uint32_t warps = gridDim.x * (kThreads / 32);
     Step k;
     const float grad_factor = a.grad_factor ? *a.grad_factor : 1.f;
     k.beta1 = a.beta1;
     k.beta2 = a.beta2;
     k.gain1 = a.one_minus_beta1 * grad_factor;
     k.gain2 = a.one_minus_beta2 * grad_factor * grad_factor;
+    k.root_beta2 = sqrtf(a.beta2);
+    k.root_gain2 = sqrtf(a.one_minus_beta2) * grad_factor;
     k.eps = a.eps;
-    uint32_t entry = 0, entry_first = 0, entry_end = 0;
-    for (uint32_t block = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); block < a.blocks; block += warps) {
-        if (block >= entry_end) {           // the tensor that this block is part of
+    uint32_t entry = 0, entry_end = 0;
+    Raw<P, G, BITS8, FORM> raw;
+    Stepped stepped;
+    for (uint32_t run = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); run < a.runs; run += gridDim.x * (kThreads / 32)) {
+        if (run >= entry_end) {             // the tensor that this run is part of
             uint32_t lo = entry, hi = a.count;
             while (hi - lo > 1) {
                 const uint32_t mid = (lo + hi) / 2;
-                if (a.entry[mid].before <= block) lo = mid; else hi = mid;
+                if (a.entry[mid].before <= run) lo = mid; else hi = mid;
             }
             entry = lo;
-            entry_first = a.entry[lo].before;
-            entry_end = lo + 1 < a.count ? a.entry[lo + 1].before : a.blocks;
+            entry_end = lo + 1 < a.count ? a.entry[lo + 1].before : a.runs;
             const uint32_t step = (uint32_t)a.steps[a.entry[lo].ordinal] + 1u;
             const float t = (float)step;
             float lr = a.entry[lo].lr;
@@ -324,11 +399,44 @@ adamw_kernel(const __grid_constant__ Args a) {
             k.rate = lr / -expm1f(t * a.ln_beta1);
             k.root_correction = rsqrtf(-expm1f(t * a.ln_beta2));
             k.key = mix(mix(a.seed + step) + a.entry[lo].ordinal);
+            k.p = a.entry[lo].p;
+            k.g = a.entry[lo].g;
+            k.first_block = a.entry[lo].first_block;
+            k.n = a.entry[lo].n;
+            k.whole = a.entry[lo].vectors ? k.n / kBlock : 0u;
         }
-        const Entry& e = a.entry[entry];
-        const uint32_t inside = block - entry_first;
-        if (e.vectors && (int64_t)(inside + 1) * kBlock <= (int64_t)e.n) step_block<P, G, BITS8, true>(a, e, k, inside, lane);
-        else step_block<P, G, BITS8, false>(a, e, k, inside, lane);
+        const uint32_t first = (run - a.entry[entry].before) * a.run, last = min(first + a.run, (k.n + kBlock - 1) / kBlock);
+        float m_scales = 0.f, r_scales = 0.f;               // lane j: of the run's block j
+        const bool scaled = BITS8 && first + lane < last;
+        if (scaled) {
+            m_scales = a.m_scale[(size_t)k.first_block + first + lane];
+            r_scales = a.v_scale[(size_t)k.first_block + first + lane];
+        }
+        bool loaded = false;
+        for (uint32_t inside = first; inside < last; ++inside) {
+            raw.m_scale = __shfl_sync(kFullMask, m_scales, inside - first);
+            raw.r_scale = __shfl_sync(kFullMask, r_scales, inside - first);
+            float m_scale = 0.f, r_scale = 0.f;
+            if (inside < k.whole) {
+                if (!loaded) load_block<P, G, BITS8, FORM, true>(a, k, inside, lane, raw);
+                compute(k, raw, stepped);
+                loaded = inside + 1 < min(last, k.whole);
+                if (loaded) load_block<P, G, BITS8, FORM, true>(a, k, inside + 1, lane, raw);
+                write<P, G, BITS8, FORM, true>(a, k, inside, lane, stepped, m_scale, r_scale);
+            } else {
+                load_block<P, G, BITS8, FORM, false>(a, k, inside, lane, raw);
+                compute(k, raw, stepped);
+                write<P, G, BITS8, FORM, false>(a, k, inside, lane, stepped, m_scale, r_scale);
+            }
+            if (BITS8 && first + lane == inside) {
+                m_scales = m_scale;
+                r_scales = r_scale;
+            }
+        }
+        if (scaled) {
+            a.m_scale[(size_t)k.first_block + first + lane] = m_scales;
+            a.v_scale[(size_t)k.first_block + first + lane] = r_scales;
+        }
     }
     // Every CTA has read the step numbers that it needed when it draws its ticket.
     __shared__ uint32_t drawn;
@@ -342,11 +450,15 @@ adamw_kernel(const __grid_constant__ Args a) {
 }
 
 using Kernel = void (*)(Args);
-template <bool BITS8>
-Kernel pick(dropit_dtype p, dropit_dtype g) {
-    if (p == DROPIT_BF16) return g == DROPIT_BF16 ? adamw_kernel<uint16_t, uint16_t, BITS8> : adamw_kernel<uint16_t, float, BITS8>;
-    return g == DROPIT_BF16 ? adamw_kernel<float, uint16_t, BITS8> : adamw_kernel<float, float, BITS8>;
+template <typename G, bool BITS8>
+Kernel pick(dropit_dtype p, int form) {
+    if (p == DROPIT_F32) return adamw_kernel<float, G, BITS8, kNearest>;
+    if (form == kMasterDither) return adamw_kernel<uint16_t, G, BITS8, kMasterDither>;
+    return form == kMaster ? adamw_kernel<uint16_t, G, BITS8, kMaster>
+           : form == kDither ? adamw_kernel<uint16_t, G, BITS8, kDither> : adamw_kernel<uint16_t, G, BITS8, kNearest>;
 }
+template <bool BITS8>
+Kernel pick(dropit_dtype p, dropit_dtype g, int form) { return g == DROPIT_BF16 ? pick<uint16_t, BITS8>(p, form) : pick<float, BITS8>(p, form); }
 
 int64_t blocks_of(int64_t n) { return (n + kBlock - 1) / kBlock; }
 
@@ -392,7 +504,6 @@ extern "C" dropit_status dropit_adamw_step(const dropit_adamw_tensor* tensors, i
     a.ln_beta2 = (float)log(o.beta2);
     a.eps = (float)o.eps;
     a.seed = mix(o.seed);
-    a.dither = o.dither && o.param_dtype == DROPIT_BF16;
     a.m = s.exp_avg;
     a.v = s.exp_avg_sq;
     a.m_scale = s.exp_avg_scale;
@@ -401,25 +512,31 @@ extern "C" dropit_status dropit_adamw_step(const dropit_adamw_tensor* tensors, i
     a.steps = s.steps;
     a.ticket = s.ticket;
     a.grad_factor = s.grad_factor;
-    const Kernel kernel = o.state_bits == 8 ? pick<true>(o.param_dtype, o.grad_dtype) : pick<false>(o.param_dtype, o.grad_dtype);
+    const int form = (o.dither ? kDither : 0) | (s.master ? kMaster : 0);
+    const Kernel kernel = o.state_bits == 8 ? pick<true>(o.param_dtype, o.grad_dtype, form) : pick<false>(o.param_dtype, o.grad_dtype, form);
+    const int64_t resident = (int64_t)sm_count() * (o.state_bits == 8 ? kResident8 : kResident32);
     int i = 0;
     while (i < count) {
         a.count = 0;
-        uint64_t blocks = 0;
+        int64_t blocks = 0;
         for (; i < count && a.count < kMaxEntries; ++i) {
             const dropit_adamw_tensor& t = tensors[i];
-            const uint64_t more = (uint64_t)blocks_of(t.n);
             if (t.n == 0) continue;
-            if (blocks + more > INT32_MAX) break;
-            Entry& e = a.entry[a.count++];
-            const uintptr_t odd = (reinterpret_cast<uintptr_t>(t.param) % (4 * param_size)) | (reinterpret_cast<uintptr_t>(t.grad) % (4 * grad_size));
-            e = {t.param, t.grad, t.lr_device, (uint32_t)t.first_block, (uint32_t)blocks, (uint32_t)t.n, (uint32_t)t.ordinal, t.lr,
-                 t.weight_decay, odd == 0 ? 1u : 0u, 0u};
-            blocks += more;
+            if (blocks + blocks_of(t.n) > INT32_MAX) break;
+            const bool vectors = (reinterpret_cast<uintptr_t>(t.param) | reinterpret_cast<uintptr_t>(t.grad)) % 16 == 0;
+            a.entry[a.count++] = {t.param, t.grad, t.lr_device, (uint32_t)t.first_block, 0u, (uint32_t)t.n, (uint32_t)t.ordinal, t.lr, t.weight_decay,
+                                  vectors ? 1u : 0u, 0u};
+            blocks += blocks_of(t.n);
         }
         if (!a.count) break;
-        a.blocks = (uint32_t)blocks;
-        const int64_t grid = std::min<int64_t>(((int64_t)blocks + kThreads / 32 - 1) / (kThreads / 32), (int64_t)sm_count() * 8);
+        a.run = kMaxRun;                                       // every warp gets two runs at least, or runs are single blocks
+        while (a.run > 1 && blocks < 2 * (int64_t)a.run * resident * (kThreads / 32)) a.run /= 2;
+        a.runs = 0;
+        for (uint32_t e = 0; e < a.count; ++e) {
+            a.entry[e].before = a.runs;
+            a.runs += (uint32_t)((blocks_of(a.entry[e].n) + a.run - 1) / a.run);
+        }
+        const int64_t grid = std::min<int64_t>((a.runs + kThreads / 32 - 1) / (kThreads / 32), resident);
         kernel<<<(unsigned)grid, kThreads, 0, as_stream(cuda_stream)>>>(a);
         const dropit_status status = check_launch();
         if (status != DROPIT_OK) return status;

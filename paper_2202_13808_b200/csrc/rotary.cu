@@ -61,9 +61,7 @@ __device__ __forceinline__ void from_float(float v, uint16_t& out) {
 __device__ __forceinline__ void from_float(float v, float& out) { out = v; }
 
 // The angle in half turns, within [-1, 1].
-__device__ __forceinline__ float half_turns(const RotaryArgs& a, int64_t offset, int pair) {
-    const int64_t at = offset + a.plan.axis[pair] * a.pos_axis;
-    const uint64_t turns = a.plan.turns[pair];
+__device__ __forceinline__ float half_turns(const RotaryArgs& a, int64_t at, uint64_t turns) {
     if (a.position_type == DROPIT_POSITION_F32) {
         const double t = (double)reinterpret_cast<const float*>(a.positions)[at] * ((double)turns * 0x1p-64);
         return (float)(2.0 * (t - rint(t)));
@@ -83,16 +81,25 @@ rotary_kernel(const __grid_constant__ RotaryArgs a) {
     const int64_t first = (int64_t)blockIdx.x * a.tokens_per_block;
     const int tokens = (int)min((int64_t)a.tokens_per_block, a.tokens - first);
     longlong4* places = reinterpret_cast<longlong4*>(angles + (a.tokens_per_block * pairs + 3) / 4 * 4);   // q in, q out, k in, k out
+    uint64_t* turns = reinterpret_cast<uint64_t*>(places + a.tokens_per_block);                          // [pairs], then the pairs' axes
+    uint8_t* axes = reinterpret_cast<uint8_t*>(turns + pairs);
+    // The plan's constants are read one address a warp: 32 different ones take 32 turns.
+    for (int j = threadIdx.x >> 5; j < pairs; j += kThreads / 32) {
+        const uint64_t t = a.plan.turns[j];
+        const uint8_t x = a.plan.axis[j];
+        if ((threadIdx.x & 31) == 0) turns[j] = t, axes[j] = x;
+    }
     for (int i = threadIdx.x; i < tokens; i += kThreads) {
         const int64_t token = first + i, batch = token / a.length, at = token - batch * a.length;
         places[i] = make_longlong4(batch * a.t[0].in_batch + at * a.t[0].in_token, batch * a.t[0].out_batch + at * a.t[0].out_token,
                                    batch * a.t[1].in_batch + at * a.t[1].in_token, batch * a.t[1].out_batch + at * a.t[1].out_token);
     }
+    __syncthreads();
     for (int i = threadIdx.x; i < tokens * pairs; i += kThreads) {
-        const int local = i / pairs;
+        const int local = i / pairs, j = i - local * pairs;
         const int64_t token = first + local, batch = token / a.length;
         float2 cs;
-        sincospif(half_turns(a, batch * a.pos_batch + (token - batch * a.length) * a.pos_token, i - local * pairs), &cs.y, &cs.x);
+        sincospif(half_turns(a, batch * a.pos_batch + (token - batch * a.length) * a.pos_token + axes[j] * a.pos_axis, turns[j]), &cs.y, &cs.x);
         cs.y *= a.sign;
         angles[i] = cs;
     }
@@ -102,6 +109,7 @@ rotary_kernel(const __grid_constant__ RotaryArgs a) {
     const int heads = a.t[0].heads + a.t[1].heads;
     using Vec = Values<T, VP>;
     using B = typename Bits<VP * sizeof(T)>::type;
+    const RotaryTensor q = a.t[0], k = a.t[1];
     for (int unit0 = 0; unit0 < units; unit0 += kThreads) {              // one round, unless a head has more units than the block threads
         const int width = min(units - unit0, kThreads), step = kThreads / width;
         const int unit = unit0 + threadIdx.x % width;
@@ -120,11 +128,10 @@ rotary_kernel(const __grid_constant__ RotaryArgs a) {
                 token[r] = local;
                 if (local < tokens) {
                     const longlong4 place = places[local];
-                    const bool key = head >= a.t[0].heads;
-                    const RotaryTensor& t = a.t[key];
-                    const int64_t h = key ? head - a.t[0].heads : head;
-                    in[r] = reinterpret_cast<const T*>(t.in) + (key ? place.z : place.x) + h * t.in_head;
-                    out[r] = reinterpret_cast<T*>(t.out) + (key ? place.w : place.y) + h * t.out_head;
+                    const bool key = head >= q.heads;
+                    const int h = key ? head - q.heads : head;
+                    in[r] = reinterpret_cast<const T*>(key ? k.in : q.in) + (key ? place.z : place.x) + h * (key ? k.in_head : q.in_head);
+                    out[r] = reinterpret_cast<T*>(key ? k.out : q.out) + (key ? place.w : place.y) + h * (key ? k.out_head : q.out_head);
                     ++live;
                     head += step;
                     while (head >= heads) head -= heads, ++local;
@@ -161,7 +168,7 @@ rotary_kernel(const __grid_constant__ RotaryArgs a) {
 
 template <typename T, int VP>
 void launch(const RotaryArgs& a, unsigned blocks, cudaStream_t stream) {
-    const size_t smem = (size_t)((a.tokens_per_block * a.plan.pairs + 3) / 4 * 4) * sizeof(float2) + (size_t)a.tokens_per_block * sizeof(longlong4);
+    const size_t smem = (size_t)((a.tokens_per_block * a.plan.pairs + 3) / 4 * 4) * sizeof(float2) + (size_t)a.tokens_per_block * sizeof(longlong4) + (size_t)a.plan.pairs * 9;
     if (a.plan.interleaved) rotary_kernel<T, VP, true><<<blocks, kThreads, smem, stream>>>(a);
     else rotary_kernel<T, VP, false><<<blocks, kThreads, smem, stream>>>(a);
 }
