@@ -6,31 +6,56 @@
 
 namespace dropit {
 
+__device__ __forceinline__ float exp2f_approx(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float rcp_approx(float x) {       // 0 above 2^126
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
 // f(a) and, if asked, f'(a).  FAST: for results that are rounded to bf16.
-template <int GATE, bool FAST>
-__device__ __forceinline__ float gate_value(float a) {
-    if constexpr (GATE == DROPIT_GATE_SILU) {
-        return FAST ? __fdividef(a, 1.f + __expf(-a)) : a / (1.f + expf(-a));
-    } else if constexpr (GATE == DROPIT_GATE_GELU) {
-        return a * (0.5f * erfcf(a * -0.70710678f));
+// The normal distribution's tail Q(|a|) = 1 - Phi(|a|) and its density's exponential e^(-a^2 / 2).  FAST: Abramowitz and Stegun 7.1.26, a polynomial in
+// 1 / (1 + 0.3275911 x), x = |a| / sqrt 2, times the exponential, off by 7.5e-8 at most; a dozen instructions where erfc takes forty.
+template <bool FAST>
+__device__ __forceinline__ float normal_tail(float a, float& e) {
+    if constexpr (FAST) {
+        e = exp2f_approx(a * (a * -0.72134752f));
+        const float t = rcp_approx(fmaf(fabsf(a), 0.23164189f, 1.f));
+        float p = fmaf(t, 0.530702715f, -0.7265760135f);
+        p = fmaf(t, p, 0.7107068705f);
+        p = fmaf(t, p, -0.142248368f);
+        p = fmaf(t, p, 0.127414796f);
+        return t * p * e;
     } else {
-        return a < 0.f ? 0.f : a;          // a NaN stays one
+        e = expf(-0.5f * a * a);
+        return 0.5f * erfcf(fabsf(a) * 0.70710678f);
     }
 }
 template <int GATE, bool FAST>
 __device__ __forceinline__ void gate_value_and_slope(float a, float& value, float& slope) {
     if constexpr (GATE == DROPIT_GATE_SILU) {
-        const float s = FAST ? __fdividef(1.f, 1.f + __expf(-a)) : 1.f / (1.f + expf(-a));
+        const float s = FAST ? rcp_approx(1.f + exp2f_approx(a * -1.44269504f)) : 1.f / (1.f + expf(-a));
         value = a * s;
-        slope = s * (1.f + a * (1.f - s));
+        slope = s * fmaf(a, 1.f - s, 1.f);
     } else if constexpr (GATE == DROPIT_GATE_GELU) {
-        const float phi = 0.5f * erfcf(a * -0.70710678f);
+        float e;
+        const float q = normal_tail<FAST>(a, e), phi = a < 0.f ? q : 1.f - q;
         value = a * phi;
-        slope = phi + a * 0.39894228f * (FAST ? __expf(-0.5f * a * a) : expf(-0.5f * a * a));
+        slope = fmaf(a * 0.39894228f, e, phi);
     } else {
-        value = a < 0.f ? 0.f : a;
+        value = a < 0.f ? 0.f : a;          // a NaN stays one
         slope = a > 0.f ? 1.f : 0.f;
     }
+}
+template <int GATE, bool FAST>
+__device__ __forceinline__ float gate_value(float a) {
+    float value, slope;
+    gate_value_and_slope<GATE, FAST>(a, value, slope);
+    return value;
 }
 
 // Tensor-core forms (bf16, C and H multiples of 8): false if the sizes are not theirs.

@@ -367,15 +367,31 @@ struct GatedLinear : public torch::autograd::Function<GatedLinear> {
         Tensor dx, dw, db;
         {
             at::AutoGradMode no_graph(false);
-            const Tensor dh = grads[0].reshape({-1, H}).to(gu.scalar_type());
-            Tensor dgu;
-            c10::optional<Tensor> sums;
-            std::tie(dgu, sums) = gated_linear_backward(dh, gu, form[1], form[2] && ctx->needs_input_grad(2));
-            if (sums.has_value()) db = *sums;
+            const Tensor dh = aligned(grads[0].reshape({-1, H}).to(gu.scalar_type()));
+            const int64_t M = gu.size(0);
+            const dropit_dtype dt = dtype_code(gu, "gu");
+            const bool bias = form[2] && ctx->needs_input_grad(2);
+            c10::cuda::CUDAGuard guard(gu.device());
+            const Tensor dgu = at::detail::empty_cuda(gu.sizes(), gu.scalar_type(), gu.device(), c10::nullopt);
+            const int64_t chunks = bias ? dropit::gated_backward_chunks(M, H, dt) : 0;
+            Tensor partial;
+            if (bias) partial = empty1(chunks * 2 * H, at::kFloat, gu);
+            if (bias || M)
+                check(dropit::gated_backward_sums(ptr(dh), ptr(gu), M, H, dt, (dropit_gate)form[1], ptr(dgu), bias ? (float*)ptr(partial) : nullptr,
+                                                  current_stream(gu)), "dropit_gated_linear_backward");
             if (ctx->needs_input_grad(0)) dx = gated_input_grad(dgu, weight).reshape(shape);
-            if (ctx->needs_input_grad(1))
-                dw = weight_grad(dgu, saved[2], saved[3], saved[4], gu.size(0) * weight.size(1), weight.size(1), ctx->saved_data["k"].toInt(),
-                                 (int)form[0], c10::nullopt, false, c10::nullopt, false).to(weight.scalar_type());
+            Tensor full;
+            if (ctx->needs_input_grad(1)) {
+                full = weight_grad(dgu, saved[2], saved[3], saved[4], M * weight.size(1), weight.size(1), ctx->saved_data["k"].toInt(), (int)form[0],
+                                   c10::nullopt, false, c10::nullopt, false);
+                dw = dt == DROPIT_F32 ? full : Tensor(at::detail::empty_cuda(full.sizes(), gu.scalar_type(), gu.device(), c10::nullopt));
+            }
+            if (bias) db = empty1(2 * H, gu.scalar_type(), gu);
+            // the bias gradient and the rounding of the weight gradient to the parameter's type
+            const bool rounds = dw.defined() && dt == DROPIT_BF16;
+            check(dropit::gated_finish(bias ? (const float*)ptr(partial) : nullptr, chunks, 2 * H, dt, bias ? ptr(db) : nullptr,
+                                       rounds ? (const float*)ptr(full) : nullptr, rounds ? ptr(dw) : nullptr, rounds ? full.numel() : 0, current_stream(gu)),
+                  "dropit_gated_linear_backward");
         }
         torch::autograd::variable_list out{dx, dw, db, Tensor(), Tensor(), Tensor()};
         if (at::GradMode::is_enabled()) {       // a and u depend on x and W: what is kept of them cannot be differentiated again
