@@ -121,6 +121,8 @@ __global__ void __launch_bounds__(32 * kFewWarps)
 gated_few_kernel(const uint16_t* __restrict__ x, const uint16_t* __restrict__ w, const uint16_t* __restrict__ bias, int M, int C, int H,
                  uint16_t* __restrict__ h, uint16_t* __restrict__ gu) {
     extern __shared__ __align__(16) float4 xs[];            // [row][first or second half of eight channels][C / 8]: lanes' loads lie side by side
+    ptx::grid_dependency_wait();
+    ptx::launch_dependents();
     const int lane = threadIdx.x & 31, j = blockIdx.x * kFewWarps + (threadIdx.x >> 5), groups = C / 8;
     const uint4* wg = reinterpret_cast<const uint4*>(w + (size_t)min(j, H - 1) * C);
     const uint4* wu = reinterpret_cast<const uint4*>(w + ((size_t)H + min(j, H - 1)) * C);
@@ -185,10 +187,10 @@ gated_few_kernel(const uint16_t* __restrict__ x, const uint16_t* __restrict__ w,
 }
 bool few_takes(int64_t M, int64_t C) { return M <= kFewRows && C % 8 == 0 && M * C <= kFewFloats; }
 template <int GATE>
-void launch_few(const void* x, const void* w, const void* bias, int M, int C, int H, void* h, void* gu, cudaStream_t stream) {
+dropit_status launch_few(const void* x, const void* w, const void* bias, int M, int C, int H, void* h, void* gu, cudaStream_t stream) {
     auto kernel = M == 1 ? gated_few_kernel<GATE, 1> : M == 2 ? gated_few_kernel<GATE, 2> : M <= 4 ? gated_few_kernel<GATE, 4> : gated_few_kernel<GATE, 8>;
-    kernel<<<(H + kFewWarps - 1) / kFewWarps, 32 * kFewWarps, (size_t)M * C * 4, stream>>>((const uint16_t*)x, (const uint16_t*)w, (const uint16_t*)bias, M, C, H,
-                                                                                        (uint16_t*)h, (uint16_t*)gu);
+    return launch_programmatic(kernel, dim3((unsigned)((H + kFewWarps - 1) / kFewWarps)), 32 * kFewWarps, (size_t)M * C * 4, stream, (const uint16_t*)x,
+                               (const uint16_t*)w, (const uint16_t*)bias, M, C, H, (uint16_t*)h, (uint16_t*)gu);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -234,6 +236,8 @@ __global__ void __launch_bounds__(kBackThreads)
 gated_backward_kernel(const T* __restrict__ dh, const T* __restrict__ gu, int64_t M, int64_t H, T* __restrict__ dgu, float* __restrict__ partial) {
     using P = Pack<T, VEC>;
     __shared__ float sums[2][kBackWarps][32 * VEC];
+    ptx::grid_dependency_wait();
+    ptx::launch_dependents();
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int64_t col = ((int64_t)blockIdx.x * 32 + lane) * VEC;
     float sg[VEC] = {}, su[VEC] = {};
@@ -280,6 +284,8 @@ template <typename T>
 __global__ void __launch_bounds__(kFinishThreads)
 finish_kernel(const float* __restrict__ partial, int chunks, int64_t cols, T* __restrict__ db, int sum_blocks, const float* __restrict__ dw,
               uint16_t* __restrict__ dw_out, int64_t count) {
+    ptx::grid_dependency_wait();
+    ptx::launch_dependents();
     if ((int)blockIdx.x < sum_blocks) {
         __shared__ float sums[kFinishThreads / 32][32];
         const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -317,11 +323,11 @@ int64_t back_chunks(int64_t M, int64_t H, dropit_dtype dtype) {
 }
 
 template <typename T, int VEC>
-void launch_backward(const void* dh, const void* gu, int64_t M, int64_t H, dropit_gate gate, void* dgu, float* partial, int64_t chunks, cudaStream_t stream) {
+dropit_status launch_backward(const void* dh, const void* gu, int64_t M, int64_t H, dropit_gate gate, void* dgu, float* partial, int64_t chunks, cudaStream_t stream) {
     const dim3 grid((unsigned)((H + 32 * VEC - 1) / (32 * VEC)), (unsigned)chunks);
     auto kernel = gate == DROPIT_GATE_SILU ? gated_backward_kernel<T, VEC, DROPIT_GATE_SILU>
                   : gate == DROPIT_GATE_GELU ? gated_backward_kernel<T, VEC, DROPIT_GATE_GELU> : gated_backward_kernel<T, VEC, DROPIT_GATE_RELU>;
-    kernel<<<grid, kBackThreads, 0, stream>>>((const T*)dh, (const T*)gu, M, H, (T*)dgu, partial);
+    return launch_programmatic(kernel, grid, kBackThreads, 0, stream, (const T*)dh, (const T*)gu, M, H, (T*)dgu, partial);
 }
 
 template <typename T>
@@ -354,14 +360,11 @@ dropit_status gated_backward_sums(const void* dh, const void* gu, int64_t M, int
     cudaStream_t stream = as_stream(cuda_stream);
     const int64_t chunks = back_chunks(M, H, dtype);
     const int vec = back_vec(H, dtype);
-    if (dtype == DROPIT_BF16) {
-        if (vec == 8) launch_backward<uint16_t, 8>(dh, gu, M, H, gate, dgu, partial, chunks, stream);
-        else launch_backward<uint16_t, 1>(dh, gu, M, H, gate, dgu, partial, chunks, stream);
-    } else {
-        if (vec == 4) launch_backward<float, 4>(dh, gu, M, H, gate, dgu, partial, chunks, stream);
-        else launch_backward<float, 1>(dh, gu, M, H, gate, dgu, partial, chunks, stream);
-    }
-    return check_launch();
+    if (dtype == DROPIT_BF16)
+        return vec == 8 ? launch_backward<uint16_t, 8>(dh, gu, M, H, gate, dgu, partial, chunks, stream)
+                        : launch_backward<uint16_t, 1>(dh, gu, M, H, gate, dgu, partial, chunks, stream);
+    return vec == 4 ? launch_backward<float, 4>(dh, gu, M, H, gate, dgu, partial, chunks, stream)
+                    : launch_backward<float, 1>(dh, gu, M, H, gate, dgu, partial, chunks, stream);
 }
 
 dropit_status gated_finish(const float* partial, int64_t chunks, int64_t cols, dropit_dtype dtype, void* db, const float* dw, void* dw_out, int64_t count,
@@ -371,11 +374,11 @@ dropit_status gated_finish(const float* partial, int64_t chunks, int64_t cols, d
     casts = std::min<int64_t>(std::max<int64_t>(casts, count ? 1 : 0), 8 * (int64_t)sm_count());
     if (sums + casts == 0) return DROPIT_OK;
     cudaStream_t stream = as_stream(cuda_stream);
+    const dim3 grid((unsigned)(sums + casts));
     if (dtype == DROPIT_BF16)
-        finish_kernel<uint16_t><<<(unsigned)(sums + casts), kFinishThreads, 0, stream>>>(partial, (int)chunks, cols, (uint16_t*)db, (int)sums, dw, (uint16_t*)dw_out, count);
-    else
-        finish_kernel<float><<<(unsigned)(sums + casts), kFinishThreads, 0, stream>>>(partial, (int)chunks, cols, (float*)db, (int)sums, dw, (uint16_t*)dw_out, count);
-    return check_launch();
+        return launch_programmatic(finish_kernel<uint16_t>, grid, kFinishThreads, 0, stream, partial, (int)chunks, cols, (uint16_t*)db, (int)sums, dw,
+                                   (uint16_t*)dw_out, count);
+    return launch_programmatic(finish_kernel<float>, grid, kFinishThreads, 0, stream, partial, (int)chunks, cols, (float*)db, (int)sums, dw, (uint16_t*)dw_out, count);
 }
 
 }  // namespace dropit
@@ -388,11 +391,9 @@ extern "C" dropit_status dropit_gated_linear(const void* x, const void* w, const
     if (sizes != DROPIT_OK || !gate_ok(gate)) return DROPIT_ERR_INVALID_ARG;
     if (M == 0) return DROPIT_OK;
     if (!buffers_ok({x, w, h}) || !is_aligned16(bias) || !is_aligned16(gu)) return DROPIT_ERR_INVALID_ARG;
-    if (dtype == DROPIT_BF16 && few_takes(M, C)) {
-        (gate == DROPIT_GATE_SILU ? launch_few<DROPIT_GATE_SILU> : gate == DROPIT_GATE_GELU ? launch_few<DROPIT_GATE_GELU> : launch_few<DROPIT_GATE_RELU>)(
+    if (dtype == DROPIT_BF16 && few_takes(M, C))
+        return (gate == DROPIT_GATE_SILU ? launch_few<DROPIT_GATE_SILU> : gate == DROPIT_GATE_GELU ? launch_few<DROPIT_GATE_GELU> : launch_few<DROPIT_GATE_RELU>)(
             x, w, bias, (int)M, (int)C, (int)H, h, gu, as_stream(cuda_stream));
-        return check_launch();
-    }
     if (dtype == DROPIT_BF16 && gated_tc_takes(M, C, H)) return gated_tc_forward(x, w, bias, M, C, H, gate, h, gu, dev_status, as_stream(cuda_stream));
     if (M > (int64_t)65535 * kTile) return DROPIT_ERR_UNSUPPORTED;
     if (dtype == DROPIT_BF16) launch_fma<uint16_t>(x, w, bias, M, C, H, gate, h, gu, as_stream(cuda_stream));

@@ -3,6 +3,7 @@
 #pragma once
 
 #include "common.cuh"
+#include "sm100_ptx.cuh"
 
 namespace dropit {
 
@@ -56,6 +57,26 @@ __device__ __forceinline__ float gate_value(float a) {
     float value, slope;
     gate_value_and_slope<GATE, FAST>(a, value, slope);
     return value;
+}
+
+// A launch that may be set up while the kernel in front of it in the stream ends: the kernel calls grid_dependency_wait before it touches memory.
+template <typename... Params, typename... Args>
+dropit_status launch_programmatic(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, cudaStream_t stream, Args... args) {
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return DROPIT_ERR_CUDA;
+    }
+    return check_launch();
 }
 
 // Tensor-core forms (bf16, C and H multiples of 8): false if the sizes are not theirs.

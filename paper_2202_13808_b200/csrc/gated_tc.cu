@@ -26,6 +26,7 @@ constexpr int kProducers = 3;                // threads that issue copies, in wa
 constexpr int kEpiWarps = 8;
 constexpr int kFirstEpiWarp = 1 + kProducers;        // warp 0: MMA
 constexpr int kThreads = 32 * (kFirstEpiWarp + kEpiWarps);
+constexpr int kSquareBytes = 32 * 64 * 2;            // through which a warp's results leave
 enum { kForward = 0, kInputGrad = 1 };
 
 constexpr int kLeftBytes = 128 * kStep * 2;
@@ -48,12 +49,12 @@ struct Control {
 };
 
 constexpr size_t smem_bytes(int mode, int bn) {
-    return 1024 + (size_t)stages(bn) * (kLeftBytes + right_bytes(mode, bn)) + sizeof(Control);
+    return 1024 + (size_t)stages(bn) * (kLeftBytes + right_bytes(mode, bn)) + (size_t)kEpiWarps * kSquareBytes + sizeof(Control);
 }
 static_assert(smem_bytes(kForward, 256) <= 227 * 1024 && smem_bytes(kForward, 128) <= 227 * 1024, "shared memory of a CTA");
 
 struct Maps {
-    CUtensorMap left, right;
+    CUtensorMap left, right, out[3];         // out: h, a, u for the TMA stores
 };
 struct Shape {
     int M, N;                                // N: hidden width (forward) or columns of dx
@@ -61,7 +62,6 @@ struct Shape {
     int splits;                              // pairs that share a tile's summed axis (the cluster has twice as many CTAs)
     uint16_t* out;                           // h or dx
     uint16_t* kept;                          // a | u, or null
-    int wide_out, wide_kept;                 // rows start on 32 bytes
     int grouped_left, grouped_right;         // one copy brings both 64-wide halves of a stage
     const uint16_t* bias;
 };
@@ -71,24 +71,35 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
-// A lane's 32 values of one row, the ones in front of `limit`, from `to` on.  32 bytes a store are whole sectors of L2 (wide: `to` is aligned to them);
-// through shared memory and TMA stores an epilogue took longer than the MMAs of a tile (70 us instead of 52 for 12608 x 768 -> 2048), waiting for
-// its staging buffers to be read.
-__device__ __forceinline__ void store_row(uint16_t* to, const float (&v)[32], int limit, bool wide) {
-    uint32_t w[16];
+// A lane's 32 values of one row into half of a square of 32 rows x 64 columns, as the TMA store's 128-byte swizzle wants them.
+__device__ __forceinline__ void stage_half(uint32_t square, int half, int lane, const float (&v)[32]) {
 #pragma unroll
-    for (int e = 0; e < 16; ++e) w[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
-    if (wide && limit >= 32) {
+    for (int c = 0; c < 4; ++c)
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(square + lane * 128 + (((4 * half + c) ^ (lane & 7)) << 4)),
+                     "r"(pack_bf16(v[8 * c], v[8 * c + 1])), "r"(pack_bf16(v[8 * c + 2], v[8 * c + 3])), "r"(pack_bf16(v[8 * c + 4], v[8 * c + 5])),
+                     "r"(pack_bf16(v[8 * c + 6], v[8 * c + 7]))
+                     : "memory");
+}
+// 32 x 32 values of a warp, a lane's row each, to rows of `pitch` elements from `to` on; `rows` and `cols` (a multiple of 8) are what there is of them.
+// They change lanes in a square of shared memory, so that a store instruction covers 64 bytes of eight rows: straight from the lanes it touches 32
+// rows, and the 96 of them a tile took longer than its MMAs; as TMA stores of such squares they crowd the unit that brings the operands.
+// (12608 x 768 -> 2048 with a and u: 80 us from the lanes, 70 by TMA, 62 so.)
+__device__ __forceinline__ void store_square(uint16_t* to, size_t pitch, uint8_t* square, int lane, const float (&v)[32], int rows, int cols) {
+    const uint32_t base = ptx::smem_u32(square);
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
-            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to + 16 * e), "r"(w[8 * e]), "r"(w[8 * e + 1]), "r"(w[8 * e + 2]),
-                         "r"(w[8 * e + 3]), "r"(w[8 * e + 4]), "r"(w[8 * e + 5]), "r"(w[8 * e + 6]), "r"(w[8 * e + 7])
-                         : "memory");
-    } else {
+    for (int c = 0; c < 4; ++c)
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(base + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4)), "r"(pack_bf16(v[8 * c], v[8 * c + 1])),
+                     "r"(pack_bf16(v[8 * c + 2], v[8 * c + 3])), "r"(pack_bf16(v[8 * c + 4], v[8 * c + 5])), "r"(pack_bf16(v[8 * c + 6], v[8 * c + 7]))
+                     : "memory");
+    __syncwarp();
+    const int c = lane & 3;
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (8 * e < limit) *reinterpret_cast<uint4*>(to + 8 * e) = make_uint4(w[4 * e], w[4 * e + 1], w[4 * e + 2], w[4 * e + 3]);
+    for (int i = 0; i < 4; ++i) {
+        const int r = 8 * i + (lane >> 2);
+        const uint4 q = *reinterpret_cast<const uint4*>(square + r * 64 + ((c ^ ((r >> 1) & 3)) << 4));
+        if (r < rows && 8 * c < cols) *reinterpret_cast<uint4*>(to + r * pitch + 8 * c) = q;
     }
+    __syncwarp();
 }
 // acc += 32 values of the bias from column c on (limit: its end)
 __device__ __forceinline__ void add_bias(float (&acc)[32], const uint16_t* bias, int c, int limit) {
@@ -116,7 +127,8 @@ gated_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Shape
     constexpr int kTmemPitch = BN <= 64 ? 64 : BN <= 128 ? 128 : 256, kColumns = 2 * kTmemPitch;
     uint8_t* left = smem;
     uint8_t* right = left + kStages * kLeftBytes;
-    Control* ctl = reinterpret_cast<Control*>(right + kStages * kRightBytes);
+    uint8_t* squares = right + kStages * kRightBytes;
+    Control* ctl = reinterpret_cast<Control*>(squares + kEpiWarps * kSquareBytes);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = ptx::cluster_ctarank(), leader = rank & ~1u;
@@ -150,7 +162,10 @@ gated_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Shape
     ptx::cluster_sync_all();             // all CTAs' barriers exist before any CTA signals another
     ptx::tc_fence_after();
     const uint32_t tmem_base = ctl->tmem_base;
+    ptx::grid_dependency_wait();         // set up while the kernel in front was ending; from here on memory is read and written
+    ptx::launch_dependents();
     const int quarter = warp & 3, half = (warp - kFirstEpiWarp) >> 2;
+    uint8_t* square = squares + (warp - kFirstEpiWarp) * kSquareBytes;     // epilogue warps
     bool final_ok = false;               // splits: this warp's accumulator is there
 
     if (warp == 0) {
@@ -253,10 +268,49 @@ gated_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Shape
             if (!ok) { *abort_flag = 1; break; }
             ptx::tc_fence_after();
             if (MODE == kInputGrad && shape.splits > 1) { final_ok = true; break; }
-            const int row = (tile / shape.tiles_n) * kRows + member * 128 + quarter * 32 + lane;
+            const int row = (tile / shape.tiles_n) * kRows + member * 128 + quarter * 32;
             const uint32_t tmem = tmem_base + ((uint32_t)(32 * quarter) << 16) + b * kTmemPitch;
             constexpr int kChunks = (MODE == kForward ? kHidden : BN) / 32;
             const int n0 = (tile % shape.tiles_n) * (MODE == kForward ? kHidden : BN);
+            if constexpr (MODE == kForward && BN % 128 == 0) {
+                // 64 columns a warp, one result after the other through the same square; the accumulator is read again for h
+                const int c0 = half * 64;
+                if (c0 < kHidden && row < shape.M && n0 + c0 < shape.N) {
+                    auto values = [&](float (&v)[32], int other, int c) {      // a or u of 32 columns
+                        uint32_t r[32];
+                        ptx::tmem_ld_32x32(tmem + other * kHidden + c, r);
+                        ptx::tmem_ld_wait();
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(r[e]);
+                        if (shape.bias) add_bias(v, shape.bias + other * shape.N, n0 + c, shape.N);
+                    };
+                    for (int result = shape.kept ? 1 : 0; result >= 0; result = result == 0 ? -1 : result == 1 ? 2 : 0) {   // a, u, h; or h
+#pragma unroll 1
+                        for (int part = 0; part < 2; ++part) {
+                            const int c = c0 + 32 * part;
+                            float v[32];
+                            values(v, result == 2, c);
+                            if (result == 0) {
+                                float u[32];
+                                values(u, 1, c);
+#pragma unroll
+                                for (int e = 0; e < 32; ++e) v[e] = gate_value<GATE, true>(v[e]) * u[e];
+                            }
+                            if (part == 0) {
+                                if (lane == 0) ptx::bulk_wait_read_all();
+                                __syncwarp();
+                            }
+                            stage_half(ptx::smem_u32(square), part, lane, v);
+                        }
+                        ptx::fence_proxy_async_smem();
+                        __syncwarp();
+                        if (lane == 0) {
+                            ptx::tma_store_2d(&maps.out[result], square, n0 + c0, row);
+                            ptx::bulk_commit();
+                        }
+                    }
+                }
+            } else
 #pragma unroll 1
             for (int ch = half; ch < kChunks; ch += 2) {
                 const int c = ch * 32;
@@ -276,31 +330,30 @@ gated_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Shape
 #pragma unroll
                     for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(r[e]);
                 }
-                if (row < shape.M && n0 + c < shape.N) {
-                    const int limit = shape.N - (n0 + c);
-                    const size_t at = (size_t)row * shape.N + n0 + c;
-                    if constexpr (MODE == kForward) {
-                        if (shape.bias) {
-                            add_bias(v, shape.bias, n0 + c, shape.N);
-                            add_bias(u, shape.bias + shape.N, n0 + c, shape.N);
-                        }
-                        if (shape.kept) {
-                            uint16_t* kept = shape.kept + at + (size_t)row * shape.N;
-                            store_row(kept, v, limit, shape.wide_kept);
-                            store_row(kept + shape.N, u, limit, shape.wide_kept);
-                        }
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) v[e] = gate_value<GATE, true>(v[e]) * u[e];
+                if (row >= shape.M || n0 + c >= shape.N) continue;
+                const int rows = shape.M - row, cols = shape.N - (n0 + c);
+                const size_t at = (size_t)row * shape.N + n0 + c;
+                if constexpr (MODE == kForward) {
+                    if (shape.bias) {
+                        add_bias(v, shape.bias, n0 + c, shape.N);
+                        add_bias(u, shape.bias + shape.N, n0 + c, shape.N);
                     }
-                    store_row(shape.out + at, v, limit, shape.wide_out);
+                    if (shape.kept) {
+                        uint16_t* kept = shape.kept + at + (size_t)row * shape.N;
+                        store_square(kept, 2 * (size_t)shape.N, square, lane, v, rows, cols);
+                        store_square(kept + shape.N, 2 * (size_t)shape.N, square, lane, u, rows, cols);
+                    }
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) v[e] = gate_value<GATE, true>(v[e]) * u[e];
                 }
-                __syncwarp();
+                store_square(shape.out + at, (size_t)shape.N, square, lane, v, rows, cols);
             }
             // the accumulator has been read: the next tile but one may have it
             ptx::tc_fence_before();
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive_cluster(drained0 + 8u * b);
         }
+        if (MODE == kForward && lane == 0) ptx::bulk_wait_all();
     }
 
     if constexpr (MODE == kInputGrad) {
@@ -330,32 +383,30 @@ gated_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Shape
             }
             ptx::cluster_sync_all();
             if (final_ok && owner == split) {
-                const int row = (first_tile / shape.tiles_n) * kRows + member * 128 + quarter * 32 + lane, n0 = (first_tile % shape.tiles_n) * BN;
+                const int row = (first_tile / shape.tiles_n) * kRows + member * 128 + quarter * 32, n0 = (first_tile % shape.tiles_n) * BN;
 #pragma unroll 1
                 for (int ch = half; ch < kChunks; ch += 2) {
                     uint32_t r[32];
                     ptx::tmem_ld_32x32(tmem + ch * 32, r);
                     ptx::tmem_ld_wait();
-                    if (row < shape.M && n0 + ch * 32 < shape.N) {
-                        float v[32];
+                    if (row >= shape.M || n0 + ch * 32 >= shape.N) continue;
+                    float v[32];
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) v[e] = 0.f;
-                        for (int s = 0; s < S; ++s) {
-                            if (s == split) {
+                    for (int e = 0; e < 32; ++e) v[e] = 0.f;
+                    for (int s = 0; s < S; ++s) {
+                        if (s == split) {
 #pragma unroll
-                                for (int e = 0; e < 32; ++e) v[e] += __uint_as_float(r[e]);
-                            } else {
-                                const uint8_t* from = smem + place(s < split ? s : s - 1, ch);
+                            for (int e = 0; e < 32; ++e) v[e] += __uint_as_float(r[e]);
+                        } else {
+                            const uint8_t* from = smem + place(s < split ? s : s - 1, ch);
 #pragma unroll
-                                for (int e = 0; e < 8; ++e) {
-                                    const float4 q = *reinterpret_cast<const float4*>(from + e * 512);
-                                    v[4 * e] += q.x; v[4 * e + 1] += q.y; v[4 * e + 2] += q.z; v[4 * e + 3] += q.w;
-                                }
+                            for (int e = 0; e < 8; ++e) {
+                                const float4 q = *reinterpret_cast<const float4*>(from + e * 512);
+                                v[4 * e] += q.x; v[4 * e + 1] += q.y; v[4 * e + 2] += q.z; v[4 * e + 3] += q.w;
                             }
                         }
-                        store_row(shape.out + (size_t)row * shape.N + n0 + ch * 32, v, shape.N - (n0 + ch * 32), shape.wide_out);
                     }
-                    __syncwarp();
+                    store_square(shape.out + (size_t)row * shape.N + n0 + ch * 32, (size_t)shape.N, square, lane, v, shape.M - row, shape.N - (n0 + ch * 32));
                 }
             }
         }
@@ -473,17 +524,19 @@ Plan plan(int mode, int64_t M, int64_t N, int64_t K) {
 }
 
 dropit_status launch(int mode, Kernel kernel, const Plan& p, const Maps& maps, const Shape& shape, int32_t* dev_status, cudaStream_t stream) {
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = 2 * p.splits;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(2 * p.splits * (p.splits > 1 ? p.tiles : std::min(p.clusters, p.tiles))));
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = smem_bytes(mode, p.width);
     cfg.stream = stream;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = 2;
     if (cudaLaunchKernelEx(&cfg, kernel, maps, shape, dev_status, spin_limit(kWaitLimit)) != cudaSuccess) {
         (void)cudaGetLastError();
         return DROPIT_ERR_CUDA;
@@ -515,10 +568,13 @@ dropit_status gated_tc_forward(const void* x, const void* w, const void* bias, i
     s.tiles = p.tiles;
     s.steps = p.steps;
     s.splits = 1;
+    if (p.width % 128 == 0) {
+        uint16_t* kept = reinterpret_cast<uint16_t*>(gu);
+        if (!make_map_out_bf16(&maps.out[0], h, M, H, H)) return DROPIT_ERR_CUDA;
+        if (gu && (!make_map_out_bf16(&maps.out[1], kept, M, H, 2 * H) || !make_map_out_bf16(&maps.out[2], kept + H, M, H, 2 * H))) return DROPIT_ERR_CUDA;
+    }
     s.out = reinterpret_cast<uint16_t*>(h);
     s.kept = reinterpret_cast<uint16_t*>(gu);
-    s.wide_out = H % 16 == 0 && reinterpret_cast<uintptr_t>(h) % 32 == 0;
-    s.wide_kept = H % 16 == 0 && reinterpret_cast<uintptr_t>(gu) % 32 == 0;
     s.bias = reinterpret_cast<const uint16_t*>(bias);
     return launch(kForward, kernel_of(kForward, p.width, gate), p, maps, s, dev_status, stream);
 }
@@ -538,7 +594,6 @@ static dropit_status input_grad_rows(const Plan& p, const uint16_t* dgu, const v
     s.steps = p.steps;
     s.splits = p.splits;
     s.out = dx;
-    s.wide_out = C % 16 == 0 && reinterpret_cast<uintptr_t>(dx) % 32 == 0;
     return launch(kInputGrad, kernel_of(kInputGrad, p.width, DROPIT_GATE_SILU), p, maps, s, dev_status, stream);
 }
 

@@ -281,6 +281,17 @@ bool make_map_2d_bf16(CUtensorMap* map, const void* base, int64_t rows, int64_t 
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool make_map_out_bf16(CUtensorMap* map, void* base, int64_t rows, int64_t cols, int64_t pitch) {
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    cuuint64_t strides[1] = {(cuuint64_t)pitch * 2};
+    cuuint32_t box[2] = {64, 32};
+    cuuint32_t estr[2] = {1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // The same matrix seen as [cols / 64][rows][64]: one box {64, box_rows, groups} brings `groups` adjacent 64-column
 // groups of box_rows rows with a single copy, laid out group after group as the MN-major operand wants them.
 // Needs cols % 64 == 0 (a partial last group would read past the end of a row).
