@@ -26,7 +26,8 @@ constexpr int kProducers = 3;                // threads that issue copies, in wa
 constexpr int kEpiWarps = 8;
 constexpr int kFirstEpiWarp = 1 + kProducers;        // warp 0: MMA
 constexpr int kThreads = 32 * (kFirstEpiWarp + kEpiWarps);
-constexpr int kSquareBytes = 32 * 64 * 2;            // through which a warp's results leave
+constexpr int kSquareBytes = 32 * 32 * 2;            // through which a warp's results leave, two of them in turn
+constexpr int kSquares = 2;
 enum { kForward = 0, kInputGrad = 1 };
 
 constexpr int kLeftBytes = 128 * kStep * 2;
@@ -49,7 +50,7 @@ struct Control {
 };
 
 constexpr size_t smem_bytes(int mode, int bn) {
-    return 1024 + (size_t)stages(bn) * (kLeftBytes + right_bytes(mode, bn)) + (size_t)kEpiWarps * kSquareBytes + sizeof(Control);
+    return 1024 + (size_t)stages(bn) * (kLeftBytes + right_bytes(mode, bn)) + (size_t)kEpiWarps * kSquares * kSquareBytes + sizeof(Control);
 }
 static_assert(smem_bytes(kForward, 256) <= 227 * 1024 && smem_bytes(kForward, 128) <= 227 * 1024, "shared memory of a CTA");
 
@@ -60,8 +61,8 @@ struct Shape {
     int M, N;                                // N: hidden width (forward) or columns of dx
     int tiles_n, tiles, steps;               // steps: stages of a tile's summed axis
     int splits;                              // pairs that share a tile's summed axis (the cluster has twice as many CTAs)
-    uint16_t* out;                           // h or dx
-    uint16_t* kept;                          // a | u, or null
+    int keep;                                // a and u are stored
+    uint16_t* out;                           // dx
     int grouped_left, grouped_right;         // one copy brings both 64-wide halves of a stage
     const uint16_t* bias;
 };
@@ -71,26 +72,18 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
-// A lane's 32 values of one row into half of a square of 32 rows x 64 columns, as the TMA store's 128-byte swizzle wants them.
-__device__ __forceinline__ void stage_half(uint32_t square, int half, int lane, const float (&v)[32]) {
+// A lane's 32 values of one row into a square of 32 x 32, as the TMA store's 64-byte swizzle wants them.
+__device__ __forceinline__ void stage_row(uint32_t square, int lane, const float (&v)[32]) {
 #pragma unroll
     for (int c = 0; c < 4; ++c)
-        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(square + lane * 128 + (((4 * half + c) ^ (lane & 7)) << 4)),
-                     "r"(pack_bf16(v[8 * c], v[8 * c + 1])), "r"(pack_bf16(v[8 * c + 2], v[8 * c + 3])), "r"(pack_bf16(v[8 * c + 4], v[8 * c + 5])),
-                     "r"(pack_bf16(v[8 * c + 6], v[8 * c + 7]))
-                     : "memory");
-}
-// 32 x 32 values of a warp, a lane's row each, to rows of `pitch` elements from `to` on; `rows` and `cols` (a multiple of 8) are what there is of them.
-// They change lanes in a square of shared memory, so that a store instruction covers 64 bytes of eight rows: straight from the lanes it touches 32
-// rows, and the 96 of them a tile took longer than its MMAs; as TMA stores of such squares they crowd the unit that brings the operands.
-// (12608 x 768 -> 2048 with a and u: 80 us from the lanes, 70 by TMA, 62 so.)
-__device__ __forceinline__ void store_square(uint16_t* to, size_t pitch, uint8_t* square, int lane, const float (&v)[32], int rows, int cols) {
-    const uint32_t base = ptx::smem_u32(square);
-#pragma unroll
-    for (int c = 0; c < 4; ++c)
-        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(base + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4)), "r"(pack_bf16(v[8 * c], v[8 * c + 1])),
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(square + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4)), "r"(pack_bf16(v[8 * c], v[8 * c + 1])),
                      "r"(pack_bf16(v[8 * c + 2], v[8 * c + 3])), "r"(pack_bf16(v[8 * c + 4], v[8 * c + 5])), "r"(pack_bf16(v[8 * c + 6], v[8 * c + 7]))
                      : "memory");
+}
+// The same square to rows of `pitch` elements from `to` on without TMA; `rows` and `cols` (a multiple of 8) are what there is of them.  The lanes change
+// places in shared memory, so that a store instruction covers 64 bytes of eight rows and not 16 of 32.
+__device__ __forceinline__ void store_square(uint16_t* to, size_t pitch, uint8_t* square, int lane, const float (&v)[32], int rows, int cols) {
+    stage_row(ptx::smem_u32(square), lane, v);
     __syncwarp();
     const int c = lane & 3;
 #pragma unroll
@@ -128,7 +121,7 @@ gated_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Shape
     uint8_t* left = smem;
     uint8_t* right = left + kStages * kLeftBytes;
     uint8_t* squares = right + kStages * kRightBytes;
-    Control* ctl = reinterpret_cast<Control*>(squares + kEpiWarps * kSquareBytes);
+    Control* ctl = reinterpret_cast<Control*>(squares + kEpiWarps * kSquares * kSquareBytes);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = ptx::cluster_ctarank(), leader = rank & ~1u;
@@ -165,7 +158,7 @@ gated_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Shape
     ptx::grid_dependency_wait();         // set up while the kernel in front was ending; from here on memory is read and written
     ptx::launch_dependents();
     const int quarter = warp & 3, half = (warp - kFirstEpiWarp) >> 2;
-    uint8_t* square = squares + (warp - kFirstEpiWarp) * kSquareBytes;     // epilogue warps
+    uint8_t* square = squares + (warp - kFirstEpiWarp) * kSquares * kSquareBytes;     // epilogue warps
     bool final_ok = false;               // splits: this warp's accumulator is there
 
     if (warp == 0) {
@@ -260,9 +253,26 @@ gated_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Shape
     } else {
         // ---------------- epilogue: accumulator -> h, a, u or dx (both CTAs, each its own 128 rows) ----------------
         const uint32_t drained0 = ptx::map_shared_to_cta(ptx::smem_u32(&ctl->drained[0]), leader);
-        int turn = 0;
+        int turn = 0, which = 0;
+        // 32 rows x 32 columns through the next of the warp's squares, once its last store has read it
+        auto store = [&](const CUtensorMap* map, const float (&v)[32], int col, int row) {
+            if (lane == 0) ptx::bulk_wait_read<kSquares - 1>();
+            __syncwarp();
+            stage_row(ptx::smem_u32(square) + which * kSquareBytes, lane, v);
+            ptx::fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+                ptx::tma_store_2d(map, square + which * kSquareBytes, col, row);
+                ptx::bulk_commit();
+            }
+            which ^= 1;
+        };
         for (int tile = first_tile; tile < shape.tiles; tile += stride, ++turn) {
             const int b = turn & 1;
+            if (MODE == kForward && shape.bias) {       // the tile's part of the bias on its way while the accumulator is not there yet
+                const int n = (tile % shape.tiles_n) * kHidden + (lane & 15) * 8;
+                if (n < shape.N) ptx::prefetch_l1(shape.bias + (lane < 16 ? 0 : shape.N) + n);
+            }
             bool ok = ptx::mbar_wait_warp(&ctl->ready[b], (uint32_t)(turn >> 1) & 1u, wait_limit);
             ok = __all_sync(kFullMask, ok && !*abort_flag);
             if (!ok) { *abort_flag = 1; break; }
@@ -272,45 +282,6 @@ gated_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Shape
             const uint32_t tmem = tmem_base + ((uint32_t)(32 * quarter) << 16) + b * kTmemPitch;
             constexpr int kChunks = (MODE == kForward ? kHidden : BN) / 32;
             const int n0 = (tile % shape.tiles_n) * (MODE == kForward ? kHidden : BN);
-            if constexpr (MODE == kForward && BN % 128 == 0) {
-                // 64 columns a warp, one result after the other through the same square; the accumulator is read again for h
-                const int c0 = half * 64;
-                if (c0 < kHidden && row < shape.M && n0 + c0 < shape.N) {
-                    auto values = [&](float (&v)[32], int other, int c) {      // a or u of 32 columns
-                        uint32_t r[32];
-                        ptx::tmem_ld_32x32(tmem + other * kHidden + c, r);
-                        ptx::tmem_ld_wait();
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(r[e]);
-                        if (shape.bias) add_bias(v, shape.bias + other * shape.N, n0 + c, shape.N);
-                    };
-                    for (int result = shape.kept ? 1 : 0; result >= 0; result = result == 0 ? -1 : result == 1 ? 2 : 0) {   // a, u, h; or h
-#pragma unroll 1
-                        for (int part = 0; part < 2; ++part) {
-                            const int c = c0 + 32 * part;
-                            float v[32];
-                            values(v, result == 2, c);
-                            if (result == 0) {
-                                float u[32];
-                                values(u, 1, c);
-#pragma unroll
-                                for (int e = 0; e < 32; ++e) v[e] = gate_value<GATE, true>(v[e]) * u[e];
-                            }
-                            if (part == 0) {
-                                if (lane == 0) ptx::bulk_wait_read_all();
-                                __syncwarp();
-                            }
-                            stage_half(ptx::smem_u32(square), part, lane, v);
-                        }
-                        ptx::fence_proxy_async_smem();
-                        __syncwarp();
-                        if (lane == 0) {
-                            ptx::tma_store_2d(&maps.out[result], square, n0 + c0, row);
-                            ptx::bulk_commit();
-                        }
-                    }
-                }
-            } else
 #pragma unroll 1
             for (int ch = half; ch < kChunks; ch += 2) {
                 const int c = ch * 32;
@@ -331,22 +302,21 @@ gated_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Shape
                     for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(r[e]);
                 }
                 if (row >= shape.M || n0 + c >= shape.N) continue;
-                const int rows = shape.M - row, cols = shape.N - (n0 + c);
-                const size_t at = (size_t)row * shape.N + n0 + c;
                 if constexpr (MODE == kForward) {
                     if (shape.bias) {
                         add_bias(v, shape.bias, n0 + c, shape.N);
                         add_bias(u, shape.bias + shape.N, n0 + c, shape.N);
                     }
-                    if (shape.kept) {
-                        uint16_t* kept = shape.kept + at + (size_t)row * shape.N;
-                        store_square(kept, 2 * (size_t)shape.N, square, lane, v, rows, cols);
-                        store_square(kept + shape.N, 2 * (size_t)shape.N, square, lane, u, rows, cols);
+                    if (shape.keep) {
+                        store(&maps.out[1], v, n0 + c, row);
+                        store(&maps.out[2], u, n0 + c, row);
                     }
 #pragma unroll
                     for (int e = 0; e < 32; ++e) v[e] = gate_value<GATE, true>(v[e]) * u[e];
+                    store(&maps.out[0], v, n0 + c, row);
+                } else {
+                    store_square(shape.out + (size_t)row * shape.N + n0 + c, (size_t)shape.N, square, lane, v, shape.M - row, shape.N - (n0 + c));
                 }
-                store_square(shape.out + at, (size_t)shape.N, square, lane, v, rows, cols);
             }
             // the accumulator has been read: the next tile but one may have it
             ptx::tc_fence_before();
@@ -568,13 +538,10 @@ dropit_status gated_tc_forward(const void* x, const void* w, const void* bias, i
     s.tiles = p.tiles;
     s.steps = p.steps;
     s.splits = 1;
-    if (p.width % 128 == 0) {
-        uint16_t* kept = reinterpret_cast<uint16_t*>(gu);
-        if (!make_map_out_bf16(&maps.out[0], h, M, H, H)) return DROPIT_ERR_CUDA;
-        if (gu && (!make_map_out_bf16(&maps.out[1], kept, M, H, 2 * H) || !make_map_out_bf16(&maps.out[2], kept + H, M, H, 2 * H))) return DROPIT_ERR_CUDA;
-    }
-    s.out = reinterpret_cast<uint16_t*>(h);
-    s.kept = reinterpret_cast<uint16_t*>(gu);
+    uint16_t* kept = reinterpret_cast<uint16_t*>(gu);
+    if (!make_map_out_bf16(&maps.out[0], h, M, H, H)) return DROPIT_ERR_CUDA;
+    if (gu && (!make_map_out_bf16(&maps.out[1], kept, M, H, 2 * H) || !make_map_out_bf16(&maps.out[2], kept + H, M, H, 2 * H))) return DROPIT_ERR_CUDA;
+    s.keep = gu != nullptr;
     s.bias = reinterpret_cast<const uint16_t*>(bias);
     return launch(kForward, kernel_of(kForward, p.width, gate), p, maps, s, dev_status, stream);
 }

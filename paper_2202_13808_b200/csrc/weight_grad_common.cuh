@@ -17,7 +17,7 @@ constexpr uint32_t kWaitLimit = 1u << 22;
 
 // Row-major bf16 matrix [rows, cols]; box = 64 columns (128 bytes) x box_rows rows, 128-byte swizzle.
 bool make_map_2d_bf16(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int box_rows);
-// For stores: rows x cols of a matrix with `pitch` elements a row; box = 64 columns x 32 rows, 128-byte swizzle.
+// For stores: rows x cols of a matrix with `pitch` elements a row; box = 32 columns x 32 rows, 64-byte swizzle.
 bool make_map_out_bf16(CUtensorMap* map, void* base, int64_t rows, int64_t cols, int64_t pitch);
 // The same matrix as [cols / 64][rows][64] (cols % 64 == 0): one box brings `groups` adjacent 64-column groups.
 bool make_map_grouped_bf16(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int groups, int box_rows);
