@@ -5,6 +5,8 @@
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/functions/basic_ops.h>
+#include <torch/csrc/autograd/functions/utils.h>
+#include <torch/csrc/autograd/saved_variable.h>
 #include <torch/extension.h>
 #include <ATen/MemoryOverlap.h>
 
@@ -272,32 +274,32 @@ GatedSizes gated_sizes(const Tensor& x, const Tensor& weight, const c10::optiona
     return s;
 }
 
-// h and, with keep, gu = a | u; both as matrices of M rows
-std::tuple<Tensor, Tensor> gated_products(const Tensor& x2, const Tensor& weight, const c10::optional<Tensor>& bias, const GatedSizes& s, int64_t gate,
-                                          bool keep) {
-    c10::cuda::CUDAGuard guard(x2.device());
-    const Tensor w = aligned(weight);
-    Tensor b;
-    if (bias.has_value() && bias->defined()) b = aligned(*bias);
-    Tensor h = at::detail::empty_cuda({s.M, s.H}, x2.scalar_type(), x2.device(), c10::nullopt), gu;
-    if (keep) gu = at::detail::empty_cuda({s.M, 2 * s.H}, x2.scalar_type(), x2.device(), c10::nullopt);
-    check(dropit_gated_linear(ptr(x2), ptr(w), b.defined() ? ptr(b) : nullptr, s.M, s.C, s.H, s.dtype, (dropit_gate)gate, ptr(h),
-                              keep ? ptr(gu) : nullptr, status_ptr(x2), current_stream(x2)), "dropit_gated_linear");
-    return {h, gu};
-}
 std::vector<int64_t> with_last(const Tensor& x, int64_t last) {
     std::vector<int64_t> shape = x.sizes().vec();
     shape.back() = last;
     return shape;
 }
+// h and, with keep, gu = a | u, in x's leading dimensions; x is laid out densely and aligned.
+std::tuple<Tensor, Tensor> gated_products(const Tensor& x, const Tensor& weight, const c10::optional<Tensor>& bias, const GatedSizes& s, int64_t gate,
+                                          bool keep) {
+    c10::cuda::CUDAGuard guard(x.device());
+    const Tensor w = aligned(weight);
+    Tensor b;
+    if (bias.has_value() && bias->defined()) b = aligned(*bias);
+    Tensor h = at::detail::empty_cuda(with_last(x, s.H), x.scalar_type(), x.device(), c10::nullopt), gu;
+    if (keep) gu = at::detail::empty_cuda(with_last(x, 2 * s.H), x.scalar_type(), x.device(), c10::nullopt);
+    check(dropit_gated_linear(ptr(x), ptr(w), b.defined() ? ptr(b) : nullptr, s.M, s.C, s.H, s.dtype, (dropit_gate)gate, ptr(h),
+                              keep ? ptr(gu) : nullptr, status_ptr(x), current_stream(x)), "dropit_gated_linear");
+    return {h, gu};
+}
 
 std::tuple<Tensor, c10::optional<Tensor>> gated_linear(const Tensor& x, const Tensor& weight, const c10::optional<Tensor>& bias, int64_t gate, bool keep) {
     const GatedSizes s = gated_sizes(x, weight, bias);
     Tensor h, gu;
-    std::tie(h, gu) = gated_products(aligned(x.reshape({s.M, s.C})), weight, bias, s, gate, keep);
+    std::tie(h, gu) = gated_products(aligned(x), weight, bias, s, gate, keep);
     c10::optional<Tensor> kept;
-    if (keep) kept = gu.reshape(with_last(x, 2 * s.H));
-    return {h.reshape(with_last(x, s.H)), kept};
+    if (keep) kept = gu;
+    return {h, kept};
 }
 
 std::tuple<Tensor, c10::optional<Tensor>> gated_linear_backward(const Tensor& dh, const Tensor& gu, int64_t gate, bool want_db) {
@@ -337,63 +339,64 @@ Tensor gated_input_grad(const Tensor& dgu, const Tensor& weight) {
     return dx;
 }
 
+bool wants(const Tensor& t) { return t.defined() && t.requires_grad(); }
+// A node that takes gradients of these tensors (made without the templates of autograd::Function, whose bookkeeping takes longer than the kernels
+// of a small layer).
+template <typename Node>
+std::shared_ptr<Node> make_node(const torch::autograd::variable_list& inputs) {
+    std::shared_ptr<Node> node(new Node(), torch::autograd::deleteNode);
+    node->set_next_edges(torch::autograd::collect_next_edges(inputs));
+    return node;
+}
+
 // The layer: x is cached as D(x) for the weight gradient (Sec. 3.2), a and u as the gate's own cache (Sec. 3.5).
-struct GatedLinear : public torch::autograd::Function<GatedLinear> {
-    static Tensor forward(torch::autograd::AutogradContext* ctx, const Tensor& x, const Tensor& weight, const c10::optional<Tensor>& bias,
-                          double gamma, int64_t fmt, int64_t gate) {
-        const GatedSizes s = gated_sizes(x, weight, bias);
-        const Tensor x2 = aligned(x.reshape({s.M, s.C}));
-        Tensor h, gu;
-        std::tie(h, gu) = gated_products(x2, weight, bias, s, gate, true);
-        const bool has_bias = bias.has_value() && bias->defined();
-        torch::autograd::variable_list saved{weight, gu};
-        if (weight.requires_grad()) {
-            Tensor values, meta, offsets;
-            int64_t k;
-            std::tie(values, meta, offsets, k) = compress(x2, gamma, (int)fmt, c10::nullopt);
-            saved.insert(saved.end(), {values, meta, offsets});
-            ctx->saved_data["k"] = k;
-        }
-        ctx->save_for_backward(saved);
-        ctx->saved_data["shape"] = x.sizes().vec();
-        ctx->saved_data["form"] = std::vector<int64_t>{fmt, gate, has_bias};
-        return h.reshape(with_last(x, s.H));
+struct GatedLinearNode : public torch::autograd::Node {
+    torch::autograd::SavedVariable weight_;
+    Tensor gu, values, meta, offsets;
+    std::vector<int64_t> shape;              // of x
+    int64_t k = 0, fmt = 0, gate = 0;
+    std::string name() const override { return "DropITGatedLinear"; }
+    void release_variables() override {
+        std::lock_guard<std::mutex> lock(mutex_);
+        weight_.reset_data();
+        gu = values = meta = offsets = Tensor();
     }
-    static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads) {
-        const auto saved = ctx->get_saved_variables();
-        const Tensor &weight = saved[0], &gu = saved[1];
-        const auto shape = ctx->saved_data["shape"].toIntVector(), form = ctx->saved_data["form"].toIntVector();
-        const int64_t H = gu.size(1) / 2;
-        Tensor dx, dw, db;
+    torch::autograd::variable_list apply(torch::autograd::variable_list&& grads) override {
+        std::lock_guard<std::mutex> lock(mutex_);
+        torch::autograd::variable_list out(3);
+        if (!grads[0].defined()) return out;
+        const Tensor weight = weight_.unpack();          // an error, if it has been released
+        const bool want_x = task_should_compute_output(0), want_w = task_should_compute_output(1), want_b = task_should_compute_output(2);
         {
             at::AutoGradMode no_graph(false);
-            const Tensor dh = aligned(grads[0].reshape({-1, H}).to(gu.scalar_type()));
-            const int64_t M = gu.size(0);
-            const dropit_dtype dt = dtype_code(gu, "gu");
-            const bool bias = form[2] && ctx->needs_input_grad(2);
             c10::cuda::CUDAGuard guard(gu.device());
-            const Tensor dgu = at::detail::empty_cuda(gu.sizes(), gu.scalar_type(), gu.device(), c10::nullopt);
-            const int64_t chunks = bias ? dropit::gated_backward_chunks(M, H, dt) : 0;
-            Tensor partial;
-            if (bias) partial = empty1(chunks * 2 * H, at::kFloat, gu);
-            if (bias || M)
-                check(dropit::gated_backward_sums(ptr(dh), ptr(gu), M, H, dt, (dropit_gate)form[1], ptr(dgu), bias ? (float*)ptr(partial) : nullptr,
+            const Tensor dh = aligned(grads[0].scalar_type() == gu.scalar_type() ? grads[0] : grads[0].to(gu.scalar_type()));
+            const int64_t H = gu.size(-1) / 2, M = gu.numel() / (2 * H);
+            const dropit_dtype dt = dtype_code(gu, "gu");
+            const Tensor dgu = at::detail::empty_cuda({M, 2 * H}, gu.scalar_type(), gu.device(), c10::nullopt);
+            const int64_t chunks = want_b ? dropit::gated_backward_chunks(M, H, dt) : 0;
+            Tensor partial, full;
+            if (want_b) partial = empty1(chunks * 2 * H, at::kFloat, gu);
+            if (want_b || M)
+                check(dropit::gated_backward_sums(ptr(dh), ptr(gu), M, H, dt, (dropit_gate)gate, ptr(dgu), want_b ? (float*)ptr(partial) : nullptr,
                                                   current_stream(gu)), "dropit_gated_linear_backward");
-            if (ctx->needs_input_grad(0)) dx = gated_input_grad(dgu, weight).reshape(shape);
-            Tensor full;
-            if (ctx->needs_input_grad(1)) {
-                full = weight_grad(dgu, saved[2], saved[3], saved[4], M * weight.size(1), weight.size(1), ctx->saved_data["k"].toInt(), (int)form[0],
-                                   c10::nullopt, false, c10::nullopt, false);
-                dw = dt == DROPIT_F32 ? full : Tensor(at::detail::empty_cuda(full.sizes(), gu.scalar_type(), gu.device(), c10::nullopt));
+            if (want_x) {
+                const Tensor w = aligned(weight);
+                out[0] = at::detail::empty_cuda(shape, gu.scalar_type(), gu.device(), c10::nullopt);
+                check(dropit_gated_input_grad(ptr(dgu), ptr(w), M, weight.size(1), H, dt, ptr(out[0]), status_ptr(gu), current_stream(gu)),
+                      "dropit_gated_input_grad");
             }
-            if (bias) db = empty1(2 * H, gu.scalar_type(), gu);
+            if (want_w) {
+                full = weight_grad(dgu, values, meta, offsets, M * weight.size(1), weight.size(1), k, (int)fmt, c10::nullopt, false, c10::nullopt, false);
+                out[1] = dt == DROPIT_F32 ? full : Tensor(at::detail::empty_cuda(full.sizes(), gu.scalar_type(), gu.device(), c10::nullopt));
+            }
+            if (want_b) out[2] = empty1(2 * H, gu.scalar_type(), gu);
             // the bias gradient and the rounding of the weight gradient to the parameter's type
-            const bool rounds = dw.defined() && dt == DROPIT_BF16;
-            check(dropit::gated_finish(bias ? (const float*)ptr(partial) : nullptr, chunks, 2 * H, dt, bias ? ptr(db) : nullptr,
-                                       rounds ? (const float*)ptr(full) : nullptr, rounds ? ptr(dw) : nullptr, rounds ? full.numel() : 0, current_stream(gu)),
+            const bool rounds = want_w && dt == DROPIT_BF16;
+            check(dropit::gated_finish(want_b ? (const float*)ptr(partial) : nullptr, chunks, 2 * H, dt, want_b ? ptr(out[2]) : nullptr,
+                                       rounds ? (const float*)ptr(full) : nullptr, rounds ? ptr(out[1]) : nullptr, rounds ? full.numel() : 0, current_stream(gu)),
                   "dropit_gated_linear_backward");
         }
-        torch::autograd::variable_list out{dx, dw, db, Tensor(), Tensor(), Tensor()};
         if (at::GradMode::is_enabled()) {       // a and u depend on x and W: what is kept of them cannot be differentiated again
             torch::autograd::variable_list given;
             std::vector<size_t> at_place;
@@ -408,7 +411,28 @@ struct GatedLinear : public torch::autograd::Function<GatedLinear> {
     }
 };
 Tensor gated_layer(const Tensor& x, const Tensor& weight, const c10::optional<Tensor>& bias, double gamma, int64_t fmt, int64_t gate) {
-    return GatedLinear::apply(x, weight, bias, gamma, fmt, gate);
+    const Tensor b = bias.has_value() ? *bias : Tensor();
+    const GatedSizes s = gated_sizes(x, weight, bias);
+    const bool records = at::GradMode::is_enabled() && (wants(x) || wants(weight) || wants(b));
+    std::shared_ptr<GatedLinearNode> node;
+    Tensor h;
+    {
+        at::AutoGradMode no_graph(false);
+        const Tensor dense = aligned(x);
+        Tensor gu;
+        std::tie(h, gu) = gated_products(dense, weight, bias, s, gate, records);
+        if (records) {
+            node = make_node<GatedLinearNode>({x, weight, b});
+            node->weight_ = torch::autograd::SavedVariable(weight, false);
+            node->gu = gu;
+            node->shape = x.sizes().vec();
+            node->fmt = fmt;
+            node->gate = gate;
+            if (weight.requires_grad()) std::tie(node->values, node->meta, node->offsets, node->k) = compress(dense, gamma, (int)fmt, c10::nullopt);
+        }
+    }
+    if (records) torch::autograd::set_history(h, node);
+    return h;
 }
 
 // ---- rotary positions ----
@@ -493,36 +517,52 @@ std::tuple<Tensor, c10::optional<Tensor>> rotary(const Tensor& q_in, const c10::
     return {q_out, second};
 }
 
+std::tuple<Tensor, c10::optional<Tensor>> rotary_layer(const Tensor& q, const c10::optional<Tensor>& k, const Tensor& positions, const Tensor& plan, bool inverse);
+
 // The gradient of a rotation is the inverse rotation, which can be differentiated again.
-struct Rotary : public torch::autograd::Function<Rotary> {
-    static torch::autograd::variable_list forward(torch::autograd::AutogradContext* ctx, const Tensor& q, const c10::optional<Tensor>& k,
-                                                  const Tensor& positions, const Tensor& plan, bool inverse) {
-        ctx->save_for_backward({positions});
-        ctx->saved_data["plan"] = plan;
-        ctx->saved_data["inverse"] = inverse;
-        ctx->saved_data["k"] = k.has_value() && k->defined();
-        Tensor q_out;
-        c10::optional<Tensor> k_out;
-        std::tie(q_out, k_out) = rotary(q, k, positions, plan, inverse, false);
-        if (k_out.has_value()) return {q_out, *k_out};
-        return {q_out};
+struct RotaryNode : public torch::autograd::Node {
+    torch::autograd::SavedVariable positions_;
+    Tensor plan;
+    bool inverse = false, has_k = false;
+    std::string name() const override { return "DropITRotary"; }
+    void release_variables() override {
+        std::lock_guard<std::mutex> lock(mutex_);
+        positions_.reset_data();
     }
-    static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads) {
-        const auto saved = ctx->get_saved_variables();
-        const Tensor plan = ctx->saved_data["plan"].toTensor();
-        const bool inverse = !ctx->saved_data["inverse"].toBool(), has_k = ctx->saved_data["k"].toBool();
-        c10::optional<Tensor> dk;
-        if (has_k) dk = grads[1];
-        const auto out = Rotary::apply(grads[0], dk, saved[0], plan, inverse);
-        return {out[0], has_k ? out[1] : Tensor(), Tensor(), Tensor(), Tensor()};
+    torch::autograd::variable_list apply(torch::autograd::variable_list&& grads) override {
+        std::lock_guard<std::mutex> lock(mutex_);
+        torch::autograd::variable_list out(2);
+        const bool q = grads[0].defined() && task_should_compute_output(0), k = has_k && grads[1].defined() && task_should_compute_output(1);
+        if (!q && !k) return out;
+        const Tensor positions = positions_.unpack();    // an error, if it has been released or changed in place
+        c10::optional<Tensor> second;
+        if (q && k) second = grads[1];
+        Tensor first;
+        std::tie(first, second) = rotary_layer(q ? grads[0] : grads[1], second, positions, plan, !inverse);
+        out[q ? 0 : 1] = first;
+        if (q && k) out[1] = *second;
+        return out;
     }
 };
 std::tuple<Tensor, c10::optional<Tensor>> rotary_layer(const Tensor& q, const c10::optional<Tensor>& k, const Tensor& positions, const Tensor& plan,
                                                        bool inverse) {
-    const auto out = Rotary::apply(q, k, positions, plan, inverse);
-    c10::optional<Tensor> second;
-    if (out.size() > 1) second = out[1];
-    return {out[0], second};
+    const bool has_k = k.has_value() && k->defined();
+    const Tensor key = has_k ? *k : Tensor();
+    if (!at::GradMode::is_enabled() || !(wants(q) || wants(key))) return rotary(q, k, positions, plan, inverse, false);
+    Tensor q_out;
+    c10::optional<Tensor> k_out;
+    {
+        at::AutoGradMode no_graph(false);
+        std::tie(q_out, k_out) = rotary(q, k, positions, plan, inverse, false);
+    }
+    auto node = make_node<RotaryNode>({q, key});
+    node->positions_ = torch::autograd::SavedVariable(positions, false);
+    node->plan = plan;
+    node->inverse = inverse;
+    node->has_k = has_k;
+    torch::autograd::set_history(q_out, node);
+    if (has_k) torch::autograd::set_history(*k_out, node);
+    return {q_out, k_out};
 }
 
 // ---- AdamW ----

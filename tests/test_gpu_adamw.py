@@ -306,3 +306,30 @@ def test_refusals(cuda_device):
     p.grad = torch.ones_like(p)
     with pytest.raises(ValueError):
         opt.step()
+
+
+def test_hooks_and_closures(cuda_device):
+    p = torch.nn.Parameter(torch.ones(8, device="cuda"))
+    opt = dropit.DropITAdamW([p], lr=1e-2)
+    calls = []
+    pre = opt.register_step_pre_hook(lambda o, args, kwargs: calls.append("pre"))
+    post = opt.register_step_post_hook(lambda o, args, kwargs: calls.append("post"))
+
+    def closure():
+        calls.append("closure")
+        opt.zero_grad()
+        loss = (p * p).sum()
+        loss.backward()
+        return loss
+    assert float(opt.step(closure)) == 8.0 and calls == ["pre", "closure", "post"]
+    pre.remove()
+    post.remove()
+    with torch.no_grad():
+        assert float(opt.step(closure)) < 8.0 and calls == ["pre", "closure", "post", "closure"]
+    schedule = torch.optim.lr_scheduler.StepLR(opt, 1, 0.5)
+    opt.step()
+    schedule.step()
+    assert opt.param_groups[0]["lr"] == 5e-3
+    version = p._version
+    opt.step()
+    assert p._version == version + 1        # autograd sees that p has changed
