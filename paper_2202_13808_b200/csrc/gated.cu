@@ -20,36 +20,68 @@ __device__ __forceinline__ void put(uint16_t* p, float v) { *p = (uint16_t)pack_
 __device__ __forceinline__ void put(float* p, float v) { *p = v; }
 
 // ---------------------------------------------------------------------------------------------
-// Products in fp32 FMA: fp32 tensors, and bf16 widths that the tensor-core kernels do not take.  64 x 64 outputs a CTA, 4 x 4 a thread
-// (two of them in the forward pass: the gate's and the other).
+// Products in fp32 FMA: fp32 tensors, and bf16 widths that the tensor-core kernels do not take.  32 x 32 outputs a CTA, so that small layers fill the SMs; its
+// four groups of 64 threads share out the summed axis, 16 of every 64 values each, 4 x 4 outputs a thread (two of them in the forward pass: the
+// gate's and the other), and add up in order at the end.  The next 64 values are on their way while these are multiplied.
+// A tile lies as [k][32] with its quads of outputs exchanged by k mod 8: conflict-free both for the transposing stores and for the reads.
+// fp32 197 x 387 -> 771 and back: forward 14 us, dx 20 (64 x 64 tiles without groups: 87 and 265).
 // ---------------------------------------------------------------------------------------------
-constexpr int kTile = 64, kStep = 16, kFmaThreads = 256;
+constexpr int kTile = 32, kStep = 64, kFmaThreads = 256, kGroups = 4;
+struct __align__(16) FmaTile {
+    float v[kStep][kTile];
+    __device__ float& at(int k, int c) { return v[k][((c >> 2) ^ (k & 7)) * 4 + (c & 3)]; }
+    __device__ float4 quad(int k, int q) const { return *reinterpret_cast<const float4*>(&v[k][(q ^ (k & 7)) * 4]); }
+};
 
-// rows x kStep of a row-major matrix [rows_total x k_total] from (row0, k0), transposed into tile[k][row]
+// kStep values of 32 rows of a row-major matrix [rows x K] from (row0, k0): 8 values x 4 rows a warp and load
 template <typename T>
-__device__ __forceinline__ void stage_rows(float (&tile)[kStep][kTile + 4], const T* a, int64_t row0, int64_t rows_total, int64_t k0, int64_t k_total) {
-    for (int i = threadIdx.x; i < kTile * kStep; i += kFmaThreads) {
-        const int k = i % kStep, r = i / kStep;
-        tile[k][r] = row0 + r < rows_total && k0 + k < k_total ? to_float(a[(row0 + r) * k_total + k0 + k]) : 0.f;
+__device__ __forceinline__ void fetch_rows(float (&r)[8], const T* a, int64_t row0, int64_t rows, int64_t k0, int64_t K) {
+    const int64_t k = k0 + (threadIdx.x >> 5) * 8 + (threadIdx.x & 7);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int64_t row = row0 + ((threadIdx.x >> 3) & 3) + 4 * j;
+        r[j] = k < K && row < rows ? to_float(a[row * K + k]) : 0.f;
     }
 }
-// kStep x cols of a row-major matrix [k_total x cols_total]
+__device__ __forceinline__ void stage_rows(FmaTile& t, const float (&r)[8]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) t.at((threadIdx.x >> 5) * 8 + (threadIdx.x & 7), ((threadIdx.x >> 3) & 3) + 4 * j) = r[j];
+}
+// kStep rows x 32 columns of a row-major matrix [K x cols]
 template <typename T>
-__device__ __forceinline__ void stage_cols(float (&tile)[kStep][kTile + 4], const T* b, int64_t k0, int64_t k_total, int64_t col0, int64_t cols_total) {
-    for (int i = threadIdx.x; i < kTile * kStep; i += kFmaThreads) {
-        const int c = i % kTile, k = i / kTile;
-        tile[k][c] = k0 + k < k_total && col0 + c < cols_total ? to_float(b[(k0 + k) * cols_total + col0 + c]) : 0.f;
+__device__ __forceinline__ void fetch_cols(float (&r)[8], const T* b, int64_t k0, int64_t K, int64_t col0, int64_t cols) {
+    const int64_t c = col0 + (threadIdx.x & 31);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int64_t k = k0 + (threadIdx.x >> 5) + 8 * j;
+        r[j] = k < K && c < cols ? to_float(b[k * cols + c]) : 0.f;
     }
 }
-__device__ __forceinline__ void multiply(float (&acc)[4][4], const float (&a)[kStep][kTile + 4], const float (&b)[kStep][kTile + 4], int ty, int tx) {
+__device__ __forceinline__ void stage_cols(FmaTile& t, const float (&r)[8]) {
 #pragma unroll
-    for (int k = 0; k < kStep; ++k) {
-        const float4 p = *reinterpret_cast<const float4*>(&a[k][ty * 4]), q = *reinterpret_cast<const float4*>(&b[k][tx * 4]);
-        const float pv[4] = {p.x, p.y, p.z, p.w}, qv[4] = {q.x, q.y, q.z, q.w};
+    for (int j = 0; j < 8; ++j) t.at((threadIdx.x >> 5) + 8 * j, threadIdx.x & 31) = r[j];
+}
+__device__ __forceinline__ void multiply(float (&acc)[4][4], const float4& p, const float4& q) {
+    const float pv[4] = {p.x, p.y, p.z, p.w}, qv[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(pv[i], qv[j], acc[i][j]);
+        for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(pv[i], qv[j], acc[i][j]);
+}
+// The groups' sums of output (r, c) of the tile for thread i's outputs i, i + 256, ..: added in the groups' order.
+__device__ __forceinline__ void join(float (&out)[4], const float (&acc)[4][4], float* room) {
+    const int group = threadIdx.x / 64, ty = (threadIdx.x / 8) % 8, tx = threadIdx.x % 8;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<float4*>(room + group * kTile * kTile + (ty * 4 + i) * kTile + tx * 4) = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+        float s = 0.f;
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) s += room[g * kTile * kTile + n * kFmaThreads + threadIdx.x];
+        out[n] = s;
     }
 }
 
@@ -57,32 +89,44 @@ template <typename T, int GATE>
 __global__ void __launch_bounds__(kFmaThreads)
 gated_fma_kernel(const T* __restrict__ x, const T* __restrict__ w, const T* __restrict__ bias, int64_t M, int64_t C, int64_t H, T* __restrict__ h,
                  T* __restrict__ gu) {
-    __shared__ __align__(16) float sa[kStep][kTile + 4], sg[kStep][kTile + 4], su[kStep][kTile + 4];
-    const int64_t row0 = (int64_t)blockIdx.y * kTile, col0 = (int64_t)blockIdx.x * kTile;
-    const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
-    float g[4][4] = {}, u[4][4] = {};
+    __shared__ FmaTile tiles[3];
+    const int64_t row0 = (int64_t)blockIdx.x * kTile, col0 = (int64_t)blockIdx.y * kTile;
+    const int group = threadIdx.x / 64, ty = (threadIdx.x / 8) % 8, tx = threadIdx.x % 8;
+    float g[4][4] = {}, u[4][4] = {}, ra[8], rg[8], ru[8];
+    fetch_rows(ra, x, row0, M, 0, C);
+    fetch_rows(rg, w, col0, H, 0, C);
+    fetch_rows(ru, w + H * C, col0, H, 0, C);
     for (int64_t k0 = 0; k0 < C; k0 += kStep) {
-        stage_rows(sa, x, row0, M, k0, C);
-        stage_rows(sg, w, col0, H, k0, C);
-        stage_rows(su, w + H * C, col0, H, k0, C);
         __syncthreads();
-        multiply(g, sa, sg, ty, tx);
-        multiply(u, sa, su, ty, tx);
+        stage_rows(tiles[0], ra);
+        stage_rows(tiles[1], rg);
+        stage_rows(tiles[2], ru);
         __syncthreads();
+        if (k0 + kStep < C) {
+            fetch_rows(ra, x, row0, M, k0 + kStep, C);
+            fetch_rows(rg, w, col0, H, k0 + kStep, C);
+            fetch_rows(ru, w + H * C, col0, H, k0 + kStep, C);
+        }
+#pragma unroll 8
+        for (int i = 0; i < kStep / kGroups; ++i) {
+            const int k = group * (kStep / kGroups) + i;
+            const float4 p = tiles[0].quad(k, ty);
+            multiply(g, p, tiles[1].quad(k, tx));
+            multiply(u, p, tiles[2].quad(k, tx));
+        }
     }
+    float gs[4], us[4];
+    join(gs, g, &tiles[0].v[0][0]);
+    join(us, u, &tiles[0].v[0][0]);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int64_t r = row0 + ty * 4 + i;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int64_t c = col0 + tx * 4 + j;
-            if (r >= M || c >= H) continue;
-            const float gv = g[i][j] + (bias ? to_float(bias[c]) : 0.f), uv = u[i][j] + (bias ? to_float(bias[H + c]) : 0.f);
-            put(h + r * H + c, gate_value<GATE, false>(gv) * uv);
-            if (gu) {
-                put(gu + r * 2 * H + c, gv);
-                put(gu + r * 2 * H + H + c, uv);
-            }
+    for (int n = 0; n < 4; ++n) {
+        const int64_t r = row0 + (n * kFmaThreads + threadIdx.x) / kTile, c = col0 + threadIdx.x % kTile;
+        if (r >= M || c >= H) continue;
+        const float gv = gs[n] + (bias ? to_float(bias[c]) : 0.f), uv = us[n] + (bias ? to_float(bias[H + c]) : 0.f);
+        put(h + r * H + c, gate_value<GATE, false>(gv) * uv);
+        if (gu) {
+            put(gu + r * 2 * H + c, gv);
+            put(gu + r * 2 * H + H + c, uv);
         }
     }
 }
@@ -90,24 +134,34 @@ gated_fma_kernel(const T* __restrict__ x, const T* __restrict__ w, const T* __re
 template <typename T>
 __global__ void __launch_bounds__(kFmaThreads)
 input_grad_fma_kernel(const T* __restrict__ dgu, const T* __restrict__ w, int64_t M, int64_t C, int64_t K, T* __restrict__ dx) {
-    __shared__ __align__(16) float sa[kStep][kTile + 4], sb[kStep][kTile + 4];
-    const int64_t row0 = (int64_t)blockIdx.y * kTile, col0 = (int64_t)blockIdx.x * kTile;
-    const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
-    float acc[4][4] = {};
+    __shared__ FmaTile tiles[2];
+    const int64_t row0 = (int64_t)blockIdx.x * kTile, col0 = (int64_t)blockIdx.y * kTile;
+    const int group = threadIdx.x / 64, ty = (threadIdx.x / 8) % 8, tx = threadIdx.x % 8;
+    float acc[4][4] = {}, ra[8], rb[8];
+    fetch_rows(ra, dgu, row0, M, 0, K);
+    fetch_cols(rb, w, 0, K, col0, C);
     for (int64_t k0 = 0; k0 < K; k0 += kStep) {
-        stage_rows(sa, dgu, row0, M, k0, K);
-        stage_cols(sb, w, k0, K, col0, C);
         __syncthreads();
-        multiply(acc, sa, sb, ty, tx);
+        stage_rows(tiles[0], ra);
+        stage_cols(tiles[1], rb);
         __syncthreads();
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int64_t r = row0 + ty * 4 + i, c = col0 + tx * 4 + j;
-            if (r < M && c < C) put(dx + r * C + c, acc[i][j]);
+        if (k0 + kStep < K) {
+            fetch_rows(ra, dgu, row0, M, k0 + kStep, K);
+            fetch_cols(rb, w, k0 + kStep, K, col0, C);
         }
+#pragma unroll 8
+        for (int i = 0; i < kStep / kGroups; ++i) {
+            const int k = group * (kStep / kGroups) + i;
+            multiply(acc, tiles[0].quad(k, ty), tiles[1].quad(k, tx));
+        }
+    }
+    float s[4];
+    join(s, acc, &tiles[0].v[0][0]);
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+        const int64_t r = row0 + (n * kFmaThreads + threadIdx.x) / kTile, c = col0 + threadIdx.x % kTile;
+        if (r < M && c < C) put(dx + r * C + c, s[n]);
+    }
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -332,7 +386,7 @@ dropit_status launch_backward(const void* dh, const void* gu, int64_t M, int64_t
 
 template <typename T>
 void launch_fma(const void* x, const void* w, const void* bias, int64_t M, int64_t C, int64_t H, dropit_gate gate, void* h, void* gu, cudaStream_t stream) {
-    const dim3 grid((unsigned)((H + kTile - 1) / kTile), (unsigned)((M + kTile - 1) / kTile));
+    const dim3 grid((unsigned)((M + kTile - 1) / kTile), (unsigned)((H + kTile - 1) / kTile));
     auto kernel = gate == DROPIT_GATE_SILU ? gated_fma_kernel<T, DROPIT_GATE_SILU>
                   : gate == DROPIT_GATE_GELU ? gated_fma_kernel<T, DROPIT_GATE_GELU> : gated_fma_kernel<T, DROPIT_GATE_RELU>;
     kernel<<<grid, kFmaThreads, 0, stream>>>((const T*)x, (const T*)w, (const T*)bias, M, C, H, (T*)h, (T*)gu);
@@ -395,7 +449,7 @@ extern "C" dropit_status dropit_gated_linear(const void* x, const void* w, const
         return (gate == DROPIT_GATE_SILU ? launch_few<DROPIT_GATE_SILU> : gate == DROPIT_GATE_GELU ? launch_few<DROPIT_GATE_GELU> : launch_few<DROPIT_GATE_RELU>)(
             x, w, bias, (int)M, (int)C, (int)H, h, gu, as_stream(cuda_stream));
     if (dtype == DROPIT_BF16 && gated_tc_takes(M, C, H)) return gated_tc_forward(x, w, bias, M, C, H, gate, h, gu, dev_status, as_stream(cuda_stream));
-    if (M > (int64_t)65535 * kTile) return DROPIT_ERR_UNSUPPORTED;
+    if (H > (int64_t)65535 * kTile) return DROPIT_ERR_UNSUPPORTED;
     if (dtype == DROPIT_BF16) launch_fma<uint16_t>(x, w, bias, M, C, H, gate, h, gu, as_stream(cuda_stream));
     else launch_fma<float>(x, w, bias, M, C, H, gate, h, gu, as_stream(cuda_stream));
     return check_launch();
@@ -426,8 +480,8 @@ extern "C" dropit_status dropit_gated_input_grad(const void* dgu, const void* w,
     if (M == 0) return DROPIT_OK;
     if (!buffers_ok({dgu, w, dx})) return DROPIT_ERR_INVALID_ARG;
     if (dtype == DROPIT_BF16 && gated_tc_takes(M, C, H)) return gated_tc_input_grad(dgu, w, M, C, H, dx, dev_status, as_stream(cuda_stream));
-    if (M > (int64_t)65535 * kTile) return DROPIT_ERR_UNSUPPORTED;
-    const dim3 grid((unsigned)((C + kTile - 1) / kTile), (unsigned)((M + kTile - 1) / kTile));
+    if (C > (int64_t)65535 * kTile) return DROPIT_ERR_UNSUPPORTED;
+    const dim3 grid((unsigned)((M + kTile - 1) / kTile), (unsigned)((C + kTile - 1) / kTile));
     if (dtype == DROPIT_BF16)
         input_grad_fma_kernel<uint16_t><<<grid, kFmaThreads, 0, as_stream(cuda_stream)>>>((const uint16_t*)dgu, (const uint16_t*)w, M, C, 2 * H, (uint16_t*)dx);
     else
