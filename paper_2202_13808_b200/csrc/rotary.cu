@@ -18,7 +18,10 @@ namespace dropit {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMaxAngles = 1024;            // angles of one block's tokens: 8 KB of shared memory
+constexpr int kMaxAngles = 640;             // angles of one block's tokens: 5 KB of shared memory
+constexpr int kMaxTokens = 64;              // of a block
+constexpr int kResident = 5;                // blocks of an SM
+constexpr int kMaxRows = 512;               // rows (token, head) whose places are looked up at a time
 
 struct RotaryTensor {
     const void* in;
@@ -37,28 +40,51 @@ struct RotaryArgs {
     dropit_rotary_plan plan;
 };
 
-template <int BYTES> struct Bits;
-template <> struct Bits<2> { using type = uint16_t; };
-template <> struct Bits<4> { using type = uint32_t; };
-template <> struct Bits<8> { using type = uint2; };
-template <> struct Bits<16> { using type = uint4; };
-
-template <typename T, int N>
-struct Values {
-    union {
-        typename Bits<N * sizeof(T)>::type bits;
-        T v[N];
-    };
-    __device__ Values() {}
+// N neighbouring values of a head in memory and as fp32.
+template <typename T, int N> struct Vec;
+template <int N> struct Vec<uint16_t, N> {
+    uint32_t w[N / 2];
+    __device__ void load(const uint16_t* p) {
+        if constexpr (N == 8) {
+            const uint4 q = *reinterpret_cast<const uint4*>(p);
+            w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
+        } else {
+            const uint2 q = *reinterpret_cast<const uint2*>(p);
+            w[0] = q.x; w[1] = q.y;
+        }
+    }
+    __device__ void store(uint16_t* p) const {
+        if constexpr (N == 8) *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+        else *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+    }
+    __device__ float get(int i) const { return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16); }
+    __device__ void set2(int i, float lo, float hi) { asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[i / 2]) : "f"(hi), "f"(lo)); }
 };
-__device__ __forceinline__ float to_float(uint16_t b) { return __uint_as_float((uint32_t)b << 16); }
-__device__ __forceinline__ float to_float(float v) { return v; }
-__device__ __forceinline__ void from_float(float v, uint16_t& out) {
-    uint16_t r;
-    asm("cvt.rn.bf16.f32 %0, %1;" : "=h"(r) : "f"(v));
-    out = r;
-}
-__device__ __forceinline__ void from_float(float v, float& out) { out = v; }
+template <> struct Vec<uint16_t, 1> {
+    uint32_t w;
+    __device__ void load(const uint16_t* p) { w = *p; }
+    __device__ void store(uint16_t* p) const { *p = (uint16_t)w; }
+    __device__ float get(int) const { return __uint_as_float(w << 16); }
+    __device__ void set(float v) { asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(0.f), "f"(v)); }
+};
+template <int N> struct Vec<float, N> {
+    float v[N];
+    __device__ void load(const float* p) {
+        if constexpr (N == 4) {
+            const float4 q = *reinterpret_cast<const float4*>(p);
+            v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
+        } else {
+            v[0] = *p;
+        }
+    }
+    __device__ void store(float* p) const {
+        if constexpr (N == 4) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+        else *p = v[0];
+    }
+    __device__ float get(int i) const { return v[i]; }
+    __device__ void set2(int i, float lo, float hi) { v[i] = lo; v[i + 1] = hi; }
+    __device__ void set(float x) { v[0] = x; }
+};
 
 // The angle in half turns, within [-1, 1].
 __device__ __forceinline__ float half_turns(const RotaryArgs& a, int64_t at, uint64_t turns) {
@@ -71,18 +97,30 @@ __device__ __forceinline__ float half_turns(const RotaryArgs& a, int64_t at, uin
     return (float)(int32_t)(((uint64_t)p * turns) >> 32) * 0x1p-31f;
 }
 
+// Where pair j of a token has its cosine and sine: two pairs are 16 bytes, and the same two of neighbouring units lie side by side, so that the units' reads
+// do not meet in the banks.
+template <int VP>
+__device__ __forceinline__ int angle_place(int j, int units) {
+    if constexpr (VP == 1) return j;
+    else return ((j % VP / 2) * units + j / VP) * 2 + (j & 1);
+}
+
 // A unit is VP pairs of one head (two vectors of VP values), or VP of the values behind the rotated ones, which are copied.  A thread keeps its
-// place in the head and steps through the rows (token, head) of the block without dividing; two rows' loads are in flight at a time.
+// place in the head and steps through the rows (token, head) of the block, whose places are looked up once for all units; two rows' loads are in
+// flight at a time, the first of them while the angles are formed.
 template <typename T, int VP, bool INTERLEAVED>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, kResident)
 rotary_kernel(const __grid_constant__ RotaryArgs a) {
-    extern __shared__ float2 angles[];                                   // [tokens][pairs], then the tokens' places
-    const int pairs = a.plan.pairs;
+    extern __shared__ __align__(16) float2 angles[];                    // [token][angle_place]
+    __shared__ ulonglong2 places[kMaxRows];                              // of a row: in, out
+    __shared__ int token_of[kMaxRows];
+    __shared__ int64_t starts[5][kMaxTokens];                            // of a token: queries in and out, keys in and out, positions
+    __shared__ uint64_t turns[DROPIT_ROTARY_MAX_PAIRS];
+    __shared__ uint8_t axes[DROPIT_ROTARY_MAX_PAIRS];
+    const int pairs = a.plan.pairs, rotating = pairs / VP, units = rotating + (a.head_dim - 2 * pairs) / VP;
     const int64_t first = (int64_t)blockIdx.x * a.tokens_per_block;
     const int tokens = (int)min((int64_t)a.tokens_per_block, a.tokens - first);
-    longlong4* places = reinterpret_cast<longlong4*>(angles + (a.tokens_per_block * pairs + 3) / 4 * 4);   // q in, q out, k in, k out
-    uint64_t* turns = reinterpret_cast<uint64_t*>(places + a.tokens_per_block);                          // [pairs], then the pairs' axes
-    uint8_t* axes = reinterpret_cast<uint8_t*>(turns + pairs);
+    const int q_heads = a.t[0].heads, heads = q_heads + a.t[1].heads, rows = tokens * heads;
     // The plan's constants are read one address a warp: 32 different ones take 32 turns.
     for (int j = threadIdx.x >> 5; j < pairs; j += kThreads / 32) {
         const uint64_t t = a.plan.turns[j];
@@ -91,76 +129,106 @@ rotary_kernel(const __grid_constant__ RotaryArgs a) {
     }
     for (int i = threadIdx.x; i < tokens; i += kThreads) {
         const int64_t token = first + i, batch = token / a.length, at = token - batch * a.length;
-        places[i] = make_longlong4(batch * a.t[0].in_batch + at * a.t[0].in_token, batch * a.t[0].out_batch + at * a.t[0].out_token,
-                                   batch * a.t[1].in_batch + at * a.t[1].in_token, batch * a.t[1].out_batch + at * a.t[1].out_token);
+        starts[0][i] = batch * a.t[0].in_batch + at * a.t[0].in_token;
+        starts[1][i] = batch * a.t[0].out_batch + at * a.t[0].out_token;
+        starts[2][i] = batch * a.t[1].in_batch + at * a.t[1].in_token;
+        starts[3][i] = batch * a.t[1].out_batch + at * a.t[1].out_token;
+        starts[4][i] = batch * a.pos_batch + at * a.pos_token;
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < tokens * pairs; i += kThreads) {
-        const int local = i / pairs, j = i - local * pairs;
-        const int64_t token = first + local, batch = token / a.length;
-        float2 cs;
-        sincospif(half_turns(a, batch * a.pos_batch + (token - batch * a.length) * a.pos_token + axes[j] * a.pos_axis, turns[j]), &cs.y, &cs.x);
-        cs.y *= a.sign;
-        angles[i] = cs;
-    }
-    __syncthreads();
-    const int rotating = pairs / VP;
-    const int units = rotating + (a.head_dim - 2 * pairs) / VP;
-    const int heads = a.t[0].heads + a.t[1].heads;
-    using Vec = Values<T, VP>;
-    using B = typename Bits<VP * sizeof(T)>::type;
-    const RotaryTensor q = a.t[0], k = a.t[1];
-    for (int unit0 = 0; unit0 < units; unit0 += kThreads) {              // one round, unless a head has more units than the block threads
-        const int width = min(units - unit0, kThreads), step = kThreads / width;
-        const int unit = unit0 + threadIdx.x % width;
-        int head = threadIdx.x / width, local = 0;
-        if (head >= step) continue;
-        const int c0 = unit >= rotating ? 2 * pairs + (unit - rotating) * VP : INTERLEAVED ? 2 * unit * VP : unit * VP;
-        const int c1 = INTERLEAVED ? c0 + VP : pairs + c0;
-        const bool copies = unit >= rotating;
-        while (head >= heads) head -= heads, ++local;
-        while (local < tokens) {
-            const T* in[2];
-            T* out[2];
-            int token[2], live = 0;
-#pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                token[r] = local;
-                if (local < tokens) {
-                    const longlong4 place = places[local];
-                    const bool key = head >= q.heads;
-                    const int h = key ? head - q.heads : head;
-                    in[r] = reinterpret_cast<const T*>(key ? k.in : q.in) + (key ? place.z : place.x) + h * (key ? k.in_head : q.in_head);
-                    out[r] = reinterpret_cast<T*>(key ? k.out : q.out) + (key ? place.w : place.y) + h * (key ? k.out_head : q.out_head);
-                    ++live;
-                    head += step;
-                    while (head >= heads) head -= heads, ++local;
-                }
+    // Quotients of up to kMaxRows rows or kMaxAngles angles: the product's error is far below half a divisor's share.
+    const float per_heads = 1.f / (float)heads, per_pairs = 1.f / (float)pairs;
+    auto look_up = [&](int row0) {
+        for (int i = threadIdx.x; i < min(kMaxRows, rows - row0); i += kThreads) {
+            const int row = row0 + i;                                    // more than kMaxRows heads come with one token a block
+            const int local = tokens == 1 ? 0 : (int)(((float)row + 0.5f) * per_heads), head = row - local * heads;
+            const T* in;
+            T* out;
+            if (head < q_heads) {
+                in = reinterpret_cast<const T*>(a.t[0].in) + starts[0][local] + head * a.t[0].in_head;
+                out = reinterpret_cast<T*>(a.t[0].out) + starts[1][local] + head * a.t[0].out_head;
+            } else {
+                in = reinterpret_cast<const T*>(a.t[1].in) + starts[2][local] + (head - q_heads) * a.t[1].in_head;
+                out = reinterpret_cast<T*>(a.t[1].out) + starts[3][local] + (head - q_heads) * a.t[1].out_head;
             }
-            Vec x[2], y[2];
-#pragma unroll
-            for (int r = 0; r < 2; ++r)
-                if (r < live) {
-                    x[r].bits = *reinterpret_cast<const B*>(in[r] + c0);
-                    if (!copies) y[r].bits = *reinterpret_cast<const B*>(in[r] + c1);
+            places[i] = make_ulonglong2(reinterpret_cast<uint64_t>(in), reinterpret_cast<uint64_t>(out));
+            token_of[i] = local;
+        }
+    };
+    bool angles_there = false;
+    for (int row0 = 0; row0 < rows; row0 += kMaxRows) {
+        if (row0) __syncthreads();
+        look_up(row0);
+        __syncthreads();
+        const int here = min(rows - row0, kMaxRows);
+        for (int unit0 = 0; unit0 < units; unit0 += kThreads) {          // one round, unless a head has more units than the block threads
+            const int width = min(units - unit0, kThreads), step = kThreads / width;
+            const int unit = unit0 + threadIdx.x % width, slot = threadIdx.x / width;
+            const bool copies = unit >= rotating;
+            const int c0 = copies ? 2 * pairs + (unit - rotating) * VP : INTERLEAVED ? 2 * unit * VP : unit * VP;
+            const int c1 = INTERLEAVED ? c0 + VP : pairs + c0;
+            Vec<T, VP> x[2], y[2];
+            uint64_t out[2];
+            int row = slot < step ? slot : here;
+            auto load = [&](int r) {
+                const int at = row + r * step;
+                if (at >= here) return;
+                const ulonglong2 place = places[at];
+                const T* in = reinterpret_cast<const T*>(place.x);
+                out[r] = place.y;
+                x[r].load(in + c0);
+                if (!copies) y[r].load(in + c1);
+            };
+            load(0);
+            load(1);
+            if (!angles_there) {
+                for (int i = threadIdx.x; i < tokens * pairs; i += kThreads) {
+                    const int local = (int)(((float)i + 0.5f) * per_pairs), j = i - local * pairs;
+                    float2 cs;
+                    sincospif(half_turns(a, starts[4][local] + axes[j] * a.pos_axis, turns[j]), &cs.y, &cs.x);
+                    cs.y *= a.sign;
+                    angles[local * pairs + angle_place<VP>(j, rotating)] = cs;
                 }
+                __syncthreads();
+                angles_there = true;
+            }
+            for (; row < here; row += 2 * step) {
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                if (r >= live) break;
-                if (!copies) {
-                    const float2* cs = angles + token[r] * pairs + unit * VP;
+                for (int r = 0; r < 2; ++r) {
+                    if (row + r * step >= here) break;
+                    T* to = reinterpret_cast<T*>(out[r]);
+                    if (!copies) {
+                        const float2* of_token = angles + token_of[row + r * step] * pairs;
+                        if constexpr (VP == 1) {
+                            const float2 cs = of_token[unit];
+                            const float u = x[r].get(0), v = y[r].get(0);
+                            x[r].set(u * cs.x - v * cs.y);
+                            y[r].set(u * cs.y + v * cs.x);
+                        } else {
 #pragma unroll
-                    for (int e = 0; e < VP; ++e) {
-                        // halves: pair e is (x[e], y[e]); neighbours: values 2e and 2e + 1 of x followed by y
-                        T& one = INTERLEAVED ? (2 * e < VP ? x[r].v[2 * e % VP] : y[r].v[2 * e % VP]) : x[r].v[e];
-                        T& two = INTERLEAVED ? (2 * e + 1 < VP ? x[r].v[(2 * e + 1) % VP] : y[r].v[(2 * e + 1) % VP]) : y[r].v[e];
-                        const float u = to_float(one), v = to_float(two);
-                        from_float(u * cs[e].x - v * cs[e].y, one);
-                        from_float(u * cs[e].y + v * cs[e].x, two);
+                            for (int e = 0; e < VP; e += 2) {
+                                const float4 cs = *reinterpret_cast<const float4*>(of_token + ((e / 2) * rotating + unit) * 2);
+                                if constexpr (INTERLEAVED) {        // pair e is two neighbours of x followed by y
+                                    Vec<T, VP>& home = 2 * e < VP ? x[r] : y[r];
+                                    const int i = 2 * e % VP;
+                                    const float u0 = home.get(i), v0 = home.get(i + 1), u1 = home.get(i + 2), v1 = home.get(i + 3);
+                                    home.set2(i, u0 * cs.x - v0 * cs.y, u0 * cs.y + v0 * cs.x);
+                                    home.set2(i + 2, u1 * cs.z - v1 * cs.w, u1 * cs.w + v1 * cs.z);
+                                } else {
+                                    const float u0 = x[r].get(e), v0 = y[r].get(e), u1 = x[r].get(e + 1), v1 = y[r].get(e + 1);
+                                    x[r].set2(e, u0 * cs.x - v0 * cs.y, u1 * cs.z - v1 * cs.w);
+                                    y[r].set2(e, u0 * cs.y + v0 * cs.x, u1 * cs.w + v1 * cs.z);
+                                }
+                            }
+                        }
+                        y[r].store(to + c1);
                     }
-                    *reinterpret_cast<B*>(out[r] + c1) = y[r].bits;
+                    x[r].store(to + c0);
                 }
-                *reinterpret_cast<B*>(out[r] + c0) = x[r].bits;
+                row += 2 * step;
+                load(0);
+                load(1);
+                row -= 2 * step;
             }
         }
     }
@@ -168,7 +236,7 @@ rotary_kernel(const __grid_constant__ RotaryArgs a) {
 
 template <typename T, int VP>
 void launch(const RotaryArgs& a, unsigned blocks, cudaStream_t stream) {
-    const size_t smem = (size_t)((a.tokens_per_block * a.plan.pairs + 3) / 4 * 4) * sizeof(float2) + (size_t)a.tokens_per_block * sizeof(longlong4) + (size_t)a.plan.pairs * 9;
+    const size_t smem = (size_t)a.tokens_per_block * a.plan.pairs * sizeof(float2);
     if (a.plan.interleaved) rotary_kernel<T, VP, true><<<blocks, kThreads, smem, stream>>>(a);
     else rotary_kernel<T, VP, false><<<blocks, kThreads, smem, stream>>>(a);
 }
@@ -262,11 +330,9 @@ extern "C" dropit_status dropit_rotary(const dropit_rotary_plan* plan, int64_t b
     int vec = 1;
     for (int n = 16 / size; n >= 4; n /= 2)
         if (takes(a, n, size)) { vec = n; break; }
-    // Four units a thread, as far as the angles fit and every SM has blocks.
-    const int64_t units = heads * ((plan->head_dim - plan->pairs) / vec);
-    int64_t per_block = (4 * kThreads + units - 1) / units;
-    per_block = std::min<int64_t>(std::min<int64_t>(per_block, kMaxAngles / plan->pairs), 256);
-    per_block = std::min<int64_t>(per_block, std::max<int64_t>(1, tokens / (2 * sm_count())));
+    // As many tokens as there is room for, in whole waves of blocks: 12608 tokens of 24 heads 17 us in one wave, 20 with a second one that is nearly empty.
+    const int64_t room = std::max<int64_t>(1, std::min<int64_t>(kMaxTokens, std::min<int64_t>(kMaxAngles / plan->pairs, kMaxRows / heads))), wave = (int64_t)kResident * sm_count();
+    const int64_t waves = (tokens + room * wave - 1) / (room * wave), per_block = (tokens + waves * wave - 1) / (waves * wave);
     a.tokens_per_block = (int)std::max<int64_t>(1, per_block);
     const int64_t blocks = (tokens + a.tokens_per_block - 1) / a.tokens_per_block;
     if (blocks > INT32_MAX) return DROPIT_ERR_UNSUPPORTED;
