@@ -157,7 +157,8 @@ __device__ __forceinline__ float2 decode_pair(uint32_t codes16) {
     const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)codes16, __NV_E4M3);
     return __half22float2(__half2(h));
 }
-// A value of less than 448 to one of the two codes around it, in the top byte and without its sign; z is the pattern of 2^-120 times the value.  There
+// A value of up to 448 (1 + 2^-20) to one of the two codes around it, in the top byte and without its sign (448 itself stays: the fraction is below one); z is
+// the pattern of 2^-120 times the value.  There
 // the 8-bit floats' normal numbers are fp32's (exponent field 1 to 15) and their subnormals fp32's subnormals, so that the code is seven bits
 // of the pattern; the 20 bits below them are the place between two codes, to which the random fraction is added.
 __device__ __forceinline__ uint32_t code_of(uint32_t z, uint32_t bits16_in_the_middle) { return (z << 4) + bits16_in_the_middle; }
@@ -175,37 +176,41 @@ __device__ __forceinline__ float approx_rcp(float x) {       // neither x nor 1 
     return r;
 }
 // Largest magnitude of the warp's values (NaN if there is one), and from it the scale.  Magnitudes below 1e-30 count as zero; a block with an infinity
-// or a NaN gets the scale NaN and stays so.  `factor` takes the values to 2^-120 of their share of 448: the scale's reciprocal, 2^-20 of itself short,
-// which keeps every share below 448 whatever the roundings, times 2^-120.  Where that product would be subnormal (magnitudes above
-// 2^14), the values take the reciprocal first.
+// or a NaN gets the scale NaN and stays so.  `factor` takes the values to 2^-120 of their share of 448, which is 448 (1 + 2^-22) at most: the scale's
+// reciprocal times 2^-120.  Where that product would be subnormal (magnitudes above 2^14), the values take the reciprocal first.
 __device__ __forceinline__ float block_scale(float top, float (&values)[8], float& factor) {
     uint32_t bits = __float_as_uint(top) & 0x7FFFFFFFu;
     bits = __reduce_max_sync(kFullMask, bits);
     const float amax = __uint_as_float(bits), scale = mul(amax, 1.f / 448.f);
     if (bits - 0x0DA24260u < 0x46800000u - 0x0DA24260u) {           // 1e-30 <= amax < 2^14
-        factor = mul(mul(approx_rcp(scale), 1.f - 0x1p-20f), 0x1p-120f);
+        factor = mul(__frcp_rn(scale), 0x1p-120f);
         return scale;
     }
     const bool none = amax < 1e-30f, bad = bits >= 0x7F800000u;
-    const float inverse = none || bad ? 0.f : mul(approx_rcp(scale), 1.f - 0x1p-20f);
+    const float inverse = none || bad ? 0.f : __frcp_rn(scale);
 #pragma unroll
     for (int i = 0; i < 8; ++i) values[i] = mul(values[i], inverse);
     factor = 0x1p-120f;
     return bad ? __uint_as_float(0x7FC00000u) : none ? 0.f : scale;
 }
 
-// FTZ: values below 2^-126 have the root 0.
-template <bool FTZ>
 __device__ __forceinline__ float approx_sqrt(float x) {
     float r;
-    if (FTZ) asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-    else asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
+// The root to the nearest fp32: x times its approximate reciprocal root, and a Newton step whose residue is exact.  Zero, infinity and NaN come out of
+// that as NaN and are their own roots; what is below 2^-126 has as good as none.
+__device__ __forceinline__ float rounded_sqrt(float x) {
+    float y;
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    const float r = mul(x, y), root = fma(fma(-r, r, x), mul(0.5f, y), r);
+    return root == root ? root : x;
+}
+
 // What holds for a tensor.
 struct Step {
     float beta1, beta2, gain1, gain2;       // gain: (1 - beta) times the gradients' factor, squared for the second moment
-    float root_beta2, root_gain2;           // their roots: moments in 8 bits hold sqrt(v)
     float eps, decay, rate, root_correction;
     uint32_t key;
     void* p;
@@ -248,7 +253,6 @@ struct Stepped {
 
 template <typename P, typename G, bool BITS8, int FORM>
 __device__ __forceinline__ void compute(const Step& k, const Raw<P, G, BITS8, FORM>& raw, Stepped& s) {
-    const float m_factor = BITS8 ? k.beta1 * raw.m_scale : k.beta1, v_factor = BITS8 ? k.root_beta2 * raw.r_scale : k.beta2;
     s.top_m = s.top_r = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
@@ -264,15 +268,19 @@ __device__ __forceinline__ void compute(const Step& k, const Raw<P, G, BITS8, FO
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const float g = value_of(raw.g, i + e);
-            const float m = fma(k.gain1, g, mul(m0[e], m_factor));
-            float v;
+            float m, v, root;
             if constexpr (BITS8) {
-                const float r = mul(v0[e], v_factor), q = mul(g, k.root_gain2);
-                v = fma(r, r, mul(q, q));
+                // every product, sum and root is rounded by itself: a code turns on the last bit, and one of a block's largest value changes all
+                // of its scale, so that another implementation in fp32 is met bit by bit or not at all
+                const float r = mul(v0[e], raw.r_scale);
+                m = mul(k.beta1, mul(m0[e], raw.m_scale)) + mul(k.gain1, g);
+                v = mul(k.beta2, mul(r, r)) + mul(mul(k.gain2, g), g);
+                root = rounded_sqrt(v);
             } else {
-                v = fma(k.gain2, mul(g, g), mul(v0[e], v_factor));
+                m = fma(k.gain1, g, mul(m0[e], k.beta1));
+                v = fma(k.gain2, mul(g, g), mul(v0[e], k.beta2));
+                root = approx_sqrt(v);
             }
-            const float root = approx_sqrt<BITS8>(v);
             const float move = mul(m, approx_rcp(fma(root, k.root_correction, k.eps)));
             s.p[i + e] = fma(value_of(raw.p, i + e), k.decay, mul(-k.rate, move));
             s.m[i + e] = m;
@@ -376,8 +384,6 @@ adamw_kernel(const __grid_constant__ Args a) {
     k.beta2 = a.beta2;
     k.gain1 = a.one_minus_beta1 * grad_factor;
     k.gain2 = a.one_minus_beta2 * grad_factor * grad_factor;
-    k.root_beta2 = sqrtf(a.beta2);
-    k.root_gain2 = sqrtf(a.one_minus_beta2) * grad_factor;
     k.eps = a.eps;
     uint32_t entry = 0, entry_end = 0;
     Raw<P, G, BITS8, FORM> raw;

@@ -170,14 +170,14 @@ gated_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Shape
             bool go = true;
             for (int tile = first_tile; tile < shape.tiles && go; tile += stride, ++turn) {
                 const int b = turn & 1;
-                if (turn >= 2 && !ptx::mbar_wait_spin(&ctl->drained[b], (uint32_t)((turn >> 1) - 1) & 1u, wait_limit)) {
+                if (turn >= 2 && !ptx::mbar_wait_poll(&ctl->drained[b], (uint32_t)((turn >> 1) - 1) & 1u, wait_limit)) {
                     *abort_flag = 1;
                     break;
                 }
                 ptx::tc_fence_after();
                 const uint32_t tmem_d = tmem_base + b * kTmemPitch;
                 for (int k = 0; k < steps; ++k) {
-                    if (*abort_flag || !ptx::mbar_wait_spin(&ctl->full[s], parity, wait_limit)) {
+                    if (*abort_flag || !ptx::mbar_wait_poll(&ctl->full[s], parity, wait_limit)) {
                         *abort_flag = 1;
                         go = false;
                         break;
@@ -213,7 +213,7 @@ gated_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Shape
                 const int n0 = (tile % shape.tiles_n) * (MODE == kForward ? kHidden : BN);
                 for (; k < steps; k += kProducers, i += kProducers) {
                     const uint32_t s = i % kStages, round = i / kStages;
-                    if (*abort_flag || (round > 0 && !ptx::mbar_wait_spin(&ctl->empty[s], (round - 1) & 1u, wait_limit))) {
+                    if (*abort_flag || (round > 0 && !ptx::mbar_wait_poll(&ctl->empty[s], (round - 1) & 1u, wait_limit))) {
                         *abort_flag = 1;
                         go = false;
                         break;

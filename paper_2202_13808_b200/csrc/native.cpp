@@ -351,21 +351,19 @@ std::shared_ptr<Node> make_node(const torch::autograd::variable_list& inputs) {
 
 // The layer: x is cached as D(x) for the weight gradient (Sec. 3.2), a and u as the gate's own cache (Sec. 3.5).
 struct GatedLinearNode : public torch::autograd::Node {
-    torch::autograd::SavedVariable weight_;
-    Tensor gu, values, meta, offsets;
+    torch::autograd::SavedVariable weight_, gu_, values_, meta_, offsets_;
     std::vector<int64_t> shape;              // of x
     int64_t k = 0, fmt = 0, gate = 0;
     std::string name() const override { return "DropITGatedLinear"; }
     void release_variables() override {
         std::lock_guard<std::mutex> lock(mutex_);
-        weight_.reset_data();
-        gu = values = meta = offsets = Tensor();
+        for (auto* v : {&weight_, &gu_, &values_, &meta_, &offsets_}) v->reset_data();
     }
     torch::autograd::variable_list apply(torch::autograd::variable_list&& grads) override {
         std::lock_guard<std::mutex> lock(mutex_);
         torch::autograd::variable_list out(3);
         if (!grads[0].defined()) return out;
-        const Tensor weight = weight_.unpack();          // an error, if it has been released
+        const Tensor weight = weight_.unpack(), gu = gu_.unpack();          // an error, if they have been released
         const bool want_x = task_should_compute_output(0), want_w = task_should_compute_output(1), want_b = task_should_compute_output(2);
         {
             at::AutoGradMode no_graph(false);
@@ -387,7 +385,7 @@ struct GatedLinearNode : public torch::autograd::Node {
                       "dropit_gated_input_grad");
             }
             if (want_w) {
-                full = weight_grad(dgu, values, meta, offsets, M * weight.size(1), weight.size(1), k, (int)fmt, c10::nullopt, false, c10::nullopt, false);
+                full = weight_grad(dgu, values_.unpack(), meta_.unpack(), offsets_.unpack(), M * weight.size(1), weight.size(1), k, (int)fmt, c10::nullopt, false, c10::nullopt, false);
                 out[1] = dt == DROPIT_F32 ? full : Tensor(at::detail::empty_cuda(full.sizes(), gu.scalar_type(), gu.device(), c10::nullopt));
             }
             if (want_b) out[2] = empty1(2 * H, gu.scalar_type(), gu);
@@ -424,11 +422,17 @@ Tensor gated_layer(const Tensor& x, const Tensor& weight, const c10::optional<Te
         if (records) {
             node = make_node<GatedLinearNode>({x, weight, b});
             node->weight_ = torch::autograd::SavedVariable(weight, false);
-            node->gu = gu;
+            node->gu_ = torch::autograd::SavedVariable(gu, false);
             node->shape = x.sizes().vec();
             node->fmt = fmt;
             node->gate = gate;
-            if (weight.requires_grad()) std::tie(node->values, node->meta, node->offsets, node->k) = compress(dense, gamma, (int)fmt, c10::nullopt);
+            if (weight.requires_grad()) {
+                const CacheTuple cache = compress(dense, gamma, (int)fmt, c10::nullopt);
+                node->values_ = torch::autograd::SavedVariable(std::get<0>(cache), false);
+                node->meta_ = torch::autograd::SavedVariable(std::get<1>(cache), false);
+                node->offsets_ = torch::autograd::SavedVariable(std::get<2>(cache), false);
+                node->k = std::get<3>(cache);
+            }
         }
     }
     if (records) torch::autograd::set_history(h, node);

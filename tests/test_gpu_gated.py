@@ -281,3 +281,56 @@ def test_refusals(cuda_device):
     for args, error in [((gu[:, :8], w), ValueError), ((gu, w.float()), TypeError), ((gu.cpu(), w), ValueError)]:
         with pytest.raises(error):
             dropit.dropit_gated_input_grad(*args)
+
+
+@pytest.mark.parametrize("M, C, H", [(4100, 1024, 1152), (200, 768, 2048)])      # many tiles a pair; pairs that share dx's summed axis
+def test_waits_that_run_out_are_reported(cuda_device, monkeypatch, M, C, H):
+    x, w, b, dh = _inputs(M, C, H, torch.bfloat16, cuda_device)
+
+    def both():
+        h, gu = dropit.dropit_gated_linear(x, w, b, keep=True)
+        return h, gu, dropit.dropit_gated_input_grad(kept, w)
+    kept = dropit.dropit_gated_linear(x, w, b, keep=True)[1]
+    good = both()
+    dropit.check_device_status(cuda_device)
+    monkeypatch.setenv("DROPIT_TEST_SPIN_LIMIT", "1")
+    timed_out = 0
+    for _ in range(3):
+        out = both()                                             # must return
+        try:
+            dropit.check_device_status(cuda_device)
+            assert all(torch.equal(p, q) for p, q in zip(out, good))
+        except dropit.DropITError as e:
+            assert e.code == 5
+            timed_out += 1
+    monkeypatch.delenv("DROPIT_TEST_SPIN_LIMIT")
+    assert all(torch.equal(p, q) for p, q in zip(both(), good))
+    dropit.check_device_status(cuda_device)
+    assert timed_out >= 1
+
+
+def test_the_graph_is_freed_and_saved_tensors_can_be_hooked(cuda_device):
+    layer = _layer(64, 32, torch.bfloat16, cuda_device, 0.9)
+    x = torch.randn(512, 64, device=cuda_device, dtype=torch.bfloat16).requires_grad_(True)
+    h = layer(x)
+    h.sum().backward()
+    with pytest.raises(RuntimeError, match="second time"):
+        h.sum().backward()
+    h = layer(x)
+    h.sum().backward(retain_graph=True)
+    h.sum().backward()
+    packed = []
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: packed.append(t.numel() * t.element_size()) or t.cpu(), lambda t: t.to(cuda_device)):
+        h = layer(x)
+    grad = x.grad.clone()
+    x.grad = None
+    h.sum().backward()
+    assert len(packed) == 5 and x.grad is not None and grad.shape == x.grad.shape
+    # what the layer holds: the gate's two projections and the cache of a tenth of x, its mask and its table, beside the weights
+    assert sum(packed) < layer.weight.numel() * 2 + 512 * 64 * 2 + 0.2 * 512 * 64 * 2 + 64
+    # a weight that changes between the passes is noticed
+    h = layer(x)
+    with torch.no_grad():
+        layer.weight.add_(1)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        h.sum().backward()
