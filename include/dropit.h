@@ -319,7 +319,8 @@ dropit_status dropit_conv_weight_grad(const void* dy, const void* values, const 
  *     column sums of the unrounded dgu (fp32, a fixed order); workspace of dropit_gated_linear_backward_workspace bytes (0 without db),
  *     contents destroyed, need not be initialised.
  *   dropit_gated_input_grad: dx [device, M x C] = dgu W (Eq. 3).
- * bf16 with C and H multiples of 8 multiplies on the tensor cores; fp32 and other widths with fp32 FMA.  M = 0 is a no-op (db is zeroed); C, H >= 1;
+ * bf16 with C and H multiples of 8 multiplies on the tensor cores, up to 8 rows of up to 12288 values in all by a kernel that reads w once; fp32 and other
+ * widths with fp32 FMA.  M = 0 is a no-op (db is zeroed); C, H >= 1;
  * M * C, M * 2H and 2H * C < 2^31 each.
  */
 typedef enum { DROPIT_GATE_SILU = 0, DROPIT_GATE_GELU = 1, DROPIT_GATE_RELU = 2 } dropit_gate;

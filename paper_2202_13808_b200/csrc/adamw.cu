@@ -175,6 +175,25 @@ __device__ __forceinline__ float approx_rcp(float x) {       // neither x nor 1 
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
+__device__ __forceinline__ float approx_sqrt(float x) {
+    float r;
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+// The root to the nearest fp32: x times its approximate reciprocal root, and a Newton step whose residue is exact.  NaN for zero, infinity and NaN, which are
+// their own roots (what is below 2^-126 has as good as none).
+__device__ __forceinline__ float rounded_sqrt(float x) {
+    float y;
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    const float r = mul(x, y);
+    return fma(fma(-r, r, x), mul(0.5f, y), r);
+}
+// The same way for the reciprocal of a scale.
+__device__ __forceinline__ float rounded_rcp(float x) {
+    const float r = approx_rcp(x);
+    return fma(fma(-x, r, 1.f), r, r);
+}
+
 // Largest magnitude of the warp's values (NaN if there is one), and from it the scale.  Magnitudes below 1e-30 count as zero; a block with an infinity
 // or a NaN gets the scale NaN and stays so.  `factor` takes the values to 2^-120 of their share of 448, which is 448 (1 + 2^-22) at most: the scale's
 // reciprocal times 2^-120.  Where that product would be subnormal (magnitudes above 2^14), the values take the reciprocal first.
@@ -183,29 +202,15 @@ __device__ __forceinline__ float block_scale(float top, float (&values)[8], floa
     bits = __reduce_max_sync(kFullMask, bits);
     const float amax = __uint_as_float(bits), scale = mul(amax, 1.f / 448.f);
     if (bits - 0x0DA24260u < 0x46800000u - 0x0DA24260u) {           // 1e-30 <= amax < 2^14
-        factor = mul(__frcp_rn(scale), 0x1p-120f);
+        factor = mul(rounded_rcp(scale), 0x1p-120f);
         return scale;
     }
     const bool none = amax < 1e-30f, bad = bits >= 0x7F800000u;
-    const float inverse = none || bad ? 0.f : __frcp_rn(scale);
+    const float inverse = none || bad ? 0.f : rounded_rcp(scale);
 #pragma unroll
     for (int i = 0; i < 8; ++i) values[i] = mul(values[i], inverse);
     factor = 0x1p-120f;
     return bad ? __uint_as_float(0x7FC00000u) : none ? 0.f : scale;
-}
-
-__device__ __forceinline__ float approx_sqrt(float x) {
-    float r;
-    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
-    return r;
-}
-// The root to the nearest fp32: x times its approximate reciprocal root, and a Newton step whose residue is exact.  Zero, infinity and NaN come out of
-// that as NaN and are their own roots; what is below 2^-126 has as good as none.
-__device__ __forceinline__ float rounded_sqrt(float x) {
-    float y;
-    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    const float r = mul(x, y), root = fma(fma(-r, r, x), mul(0.5f, y), r);
-    return root == root ? root : x;
 }
 
 // What holds for a tensor.
@@ -251,8 +256,9 @@ struct Stepped {
     float top_m, top_r;         // largest magnitudes
 };
 
-template <typename P, typename G, bool BITS8, int FORM>
-__device__ __forceinline__ void compute(const Step& k, const Raw<P, G, BITS8, FORM>& raw, Stepped& s) {
+// ANY: roots of zero, infinity and NaN too; without it they come out as NaN, in s.top_r as well.
+template <bool ANY, typename P, typename G, bool BITS8, int FORM>
+__device__ __forceinline__ void compute_as(const Step& k, const Raw<P, G, BITS8, FORM>& raw, Stepped& s) {
     s.top_m = s.top_r = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
@@ -276,6 +282,7 @@ __device__ __forceinline__ void compute(const Step& k, const Raw<P, G, BITS8, FO
                 m = mul(k.beta1, mul(m0[e], raw.m_scale)) + mul(k.gain1, g);
                 v = mul(k.beta2, mul(r, r)) + mul(mul(k.gain2, g), g);
                 root = rounded_sqrt(v);
+                if (ANY && root != root) root = v;
             } else {
                 m = fma(k.gain1, g, mul(m0[e], k.beta1));
                 v = fma(k.gain2, mul(g, g), mul(v0[e], k.beta2));
@@ -291,6 +298,12 @@ __device__ __forceinline__ void compute(const Step& k, const Raw<P, G, BITS8, FO
             s.top_r = max_nan(s.top_r, s.v[i], s.v[i + 1]);
         }
     }
+}
+
+template <typename P, typename G, bool BITS8, int FORM>
+__device__ __forceinline__ void compute(const Step& k, const Raw<P, G, BITS8, FORM>& raw, Stepped& s) {
+    compute_as<false>(k, raw, s);
+    if (BITS8 && s.top_r != s.top_r) compute_as<true>(k, raw, s);
 }
 
 template <typename P, typename G, bool BITS8, int FORM, bool FULL>
