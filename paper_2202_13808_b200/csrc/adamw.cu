@@ -28,10 +28,10 @@ namespace dropit {
 namespace {
 
 constexpr int kBlock = DROPIT_ADAMW_BLOCK;
-constexpr int kThreads = 256;
+constexpr int kThreads = 128;
 constexpr int kMaxEntries = 512;
-constexpr uint32_t kMaxRun = 8;                     // blocks of a run: a sector of scales
-constexpr int kResident8 = 3, kResident32 = 2;          // CTAs per SM: 8 bits 199 / 187 / 226 us with 2 / 3 / 4 (the last spills), 32 bits 387 / 390 with 2 / 3
+constexpr uint32_t kMaxRun = 16;                    // blocks of a run (8 bits 213 / 205 / 202 us with 8 / 16 / 32)
+constexpr int kResident8 = 5, kResident32 = 4;          // CTAs per SM: 8 bits 216 / 205 / 227 us with 4 / 5 / 6, which spills
 
 struct Entry {
     void* p;
@@ -385,7 +385,7 @@ __device__ __forceinline__ void write(const Args& a, const Step& k, uint32_t ins
 
 // Warps take runs of a tensor's blocks in turn (a.run of them, fewer where that leaves warps without any), so that the tensor's constants are
 // looked up and the scales of a run come and go once; the next block's loads are under way while one is rounded and written.
-// 85 M bf16 values with moments in 8 bits: 187 us; 268 with single blocks dealt out (nearly every one another tensor's), 295 with one stretch of
+// 85 M bf16 values with moments in 8 bits: 205 us; 268 with single blocks dealt out (nearly every one another tensor's), 295 with one stretch of
 // blocks a CTA, whose streams keep in step.
 template <typename P, typename G, bool BITS8, int FORM>
 __global__ void __launch_bounds__(kThreads, BITS8 ? kResident8 : kResident32)

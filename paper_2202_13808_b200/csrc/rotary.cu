@@ -170,8 +170,7 @@ rotary_kernel(const __grid_constant__ RotaryArgs a) {
             Vec<T, VP> x[2], y[2];
             uint64_t out[2];
             int row = slot < step ? slot : here;
-            auto load = [&](int r) {
-                const int at = row + r * step;
+            auto load = [&](int r, int at) {
                 if (at >= here) return;
                 const ulonglong2 place = places[at];
                 const T* in = reinterpret_cast<const T*>(place.x);
@@ -179,8 +178,8 @@ rotary_kernel(const __grid_constant__ RotaryArgs a) {
                 x[r].load(in + c0);
                 if (!copies) y[r].load(in + c1);
             };
-            load(0);
-            load(1);
+            load(0, row);
+            load(1, row + step);
             if (!angles_there) {
                 for (int i = threadIdx.x; i < tokens * pairs; i += kThreads) {
                     const int local = (int)(((float)i + 0.5f) * per_pairs), j = i - local * pairs;
@@ -195,7 +194,7 @@ rotary_kernel(const __grid_constant__ RotaryArgs a) {
             for (; row < here; row += 2 * step) {
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
-                    if (row + r * step >= here) break;
+                    if (row + r * step >= here) continue;
                     T* to = reinterpret_cast<T*>(out[r]);
                     if (!copies) {
                         const float2* of_token = angles + token_of[row + r * step] * pairs;
@@ -224,11 +223,8 @@ rotary_kernel(const __grid_constant__ RotaryArgs a) {
                         y[r].store(to + c1);
                     }
                     x[r].store(to + c0);
+                    load(r, row + (2 + r) * step);       // on its way while the other row is turned
                 }
-                row += 2 * step;
-                load(0);
-                load(1);
-                row -= 2 * step;
             }
         }
     }
