@@ -45,7 +45,7 @@ struct Control {
     int abort_flag;
     int consumed;                            // leader: stages whose operands the MMA thread has seen arrive
     int issued[4];                           // per slot: rounds this CTA's producers have issued
-    int peer_issued[4];                      // leader: the other CTA's
+    int peer_issued[4];                      // the other CTA's
     int peer_abort;
 };
 
@@ -323,7 +323,7 @@ gated_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Shape
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive_cluster(drained0 + 8u * b);
         }
-        if (MODE == kForward && lane == 0) ptx::bulk_wait_all();
+        if (MODE == kForward && lane == 0) ptx::bulk_wait_read<0>();     // the squares have been read; what they hold arrives before the kernel counts as ended
     }
 
     if constexpr (MODE == kInputGrad) {
@@ -382,39 +382,42 @@ gated_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Shape
         }
     }
 
-    // Neither CTA leaves while another may still signal its barriers or read its shared memory.  After a wait was given up, copies may be in
-    // flight whose stage the MMA thread never took, and one CTA may have issued a stage that the other did not: the leader squares the accounts
-    // of those barriers by hand (bytes that were announced but never sent are counted as arrived; bytes that were sent unannounced get
-    // their arrival) and waits for the rest, between two cluster barriers that keep the other CTA alive.
+    // Neither CTA leaves while another may still signal its barriers or read its shared memory.
     __syncthreads();
-    if (member && threadIdx.x == 0) {
+    if (threadIdx.x == 0) {
+        const uint32_t other = rank ^ 1u;
+        ptx::st_cluster_u32(ptx::map_shared_to_cta(ptx::smem_u32(&ctl->peer_abort), other), (uint32_t)*abort_flag);
         for (int s = 0; s < kStages; ++s)
-            ptx::st_cluster_u32(ptx::map_shared_to_cta(ptx::smem_u32(&ctl->peer_issued[s]), leader), (uint32_t)ctl->issued[s]);
-        if (*abort_flag) ptx::st_cluster_u32(ptx::map_shared_to_cta(ptx::smem_u32(&ctl->peer_abort), leader), 1u);
-    }
-    ptx::cluster_sync_all();
-    if (!member && threadIdx.x == 0 && (*abort_flag || *reinterpret_cast<volatile int*>(&ctl->peer_abort))) {
-        *abort_flag = 1;
-        const int consumed = ctl->consumed;
-        for (int s = 0; s < kStages; ++s) {
-            const int taken = consumed > s ? (consumed - s + kStages - 1) / kStages : 0;      // rounds of slot s that the MMAs took
-            const int ours = ctl->issued[s], theirs = *reinterpret_cast<volatile int*>(&ctl->peer_issued[s]);
-            if (ours <= taken && theirs <= taken) continue;
-            uint64_t* bar = &ctl->full[s];
-            if (ours <= taken) ptx::mbar_arrive_expect_tx(bar, kStageTx);
-            else if (theirs <= taken) ptx::mbar_complete_tx(bar, kStageTx);
-            ptx::mbar_wait(bar, (uint32_t)taken & 1u, kWaitLimit);
-        }
+            ptx::st_cluster_u32(ptx::map_shared_to_cta(ptx::smem_u32(&ctl->peer_issued[s]), other), (uint32_t)ctl->issued[s]);
     }
     ptx::tc_fence_before();
     ptx::cluster_sync_all();
+    if (*abort_flag || *reinterpret_cast<volatile int*>(&ctl->peer_abort)) {
+        // After a wait was given up, copies may be in flight whose stage the MMA thread never took, and one CTA may have issued a stage that the
+        // other did not: the leader squares the accounts of those barriers by hand (bytes that were announced but never sent are counted as
+        // arrived; bytes that were sent unannounced get their arrival) and waits for the rest, while the other CTA stays.
+        if (!member && threadIdx.x == 0) {
+            const int consumed = ctl->consumed;
+            for (int s = 0; s < kStages; ++s) {
+                const int taken = consumed > s ? (consumed - s + kStages - 1) / kStages : 0;      // rounds of slot s that the MMAs took
+                const int ours = ctl->issued[s], theirs = *reinterpret_cast<volatile int*>(&ctl->peer_issued[s]);
+                if (ours <= taken && theirs <= taken) continue;
+                uint64_t* bar = &ctl->full[s];
+                if (ours <= taken) ptx::mbar_arrive_expect_tx(bar, kStageTx);
+                else if (theirs <= taken) ptx::mbar_complete_tx(bar, kStageTx);
+                ptx::mbar_wait(bar, (uint32_t)taken & 1u, kWaitLimit);
+            }
+            if (dev_status) atomicExch(dev_status, (int)DROPIT_ERR_TIMEOUT);
+        }
+        __syncthreads();
+        ptx::cluster_sync_all();         // both CTAs of the pair come here (others of the cluster may have left)
+    }
     if (warp == 0) {
         // tensor memory is given back by both CTAs, and only once no MMA can still write to it
         ptx::mbar_wait_warp(&ctl->done, 0, kWaitLimit);
         ptx::tc_fence_after();
         ptx::tmem_dealloc_pair(tmem_base, kColumns);
     }
-    if (*abort_flag && threadIdx.x == 0 && dev_status) atomicExch(dev_status, (int)DROPIT_ERR_TIMEOUT);
 }
 
 using Kernel = void (*)(Maps, Shape, int32_t*, uint32_t);
@@ -457,7 +460,8 @@ struct Plan {
 // below it.
 float step_us(int mode, int width) { return 1.14e-5f * (float)(kLeftBytes + right_bytes(mode, width)); }
 
-// Width of the tiles and, for dx, pairs per tile: whatever is done first.  A wave costs its stages; the joining of two or four pairs about 2 us.
+// Width of the tiles and, for dx, pairs per tile: whatever is done first.  A wave costs its stages, the last tile's epilogue 2.6 us at the full width; pairs
+// that join their sums 1 us for the cluster's barriers and 9 at the full width for sending and adding (measured with %globaltimer).
 Plan plan(int mode, int64_t M, int64_t N, int64_t K) {
     static std::atomic<int> pairs_of[64][3];                // [device][log2 splits]
     const int dev = current_device();
@@ -486,7 +490,7 @@ Plan plan(int mode, int64_t M, int64_t N, int64_t K) {
             p.clusters = resident[l];
             if (l && (p.tiles > p.clusters || p.steps < 4 * p.splits)) break;       // one tile a cluster, and enough to share
             const int waves = (p.tiles + p.clusters - 1) / p.clusters;
-            p.us = (float)(waves * ((p.steps + p.splits - 1) / p.splits)) * step_us(mode, w) + (l ? 2.f : 0.f);
+            p.us = (float)(waves * ((p.steps + p.splits - 1) / p.splits)) * step_us(mode, w) + (l ? 1.f + 0.035f * (float)w : 0.01f * (float)w);
             if (!best.width || p.us < best.us * 0.98f) best = p;
         }
     }
@@ -574,7 +578,7 @@ dropit_status gated_tc_input_grad(const void* dgu, const void* w, int64_t M, int
         const int64_t rows = (int64_t)kRows * (whole.tiles / whole.clusters * whole.clusters / whole.tiles_n);
         if (rows > 0 && rows < M) {
             const Plan first = plan(kInputGrad, rows, C, 2 * H), rest = plan(kInputGrad, M - rows, C, 2 * H);
-            constexpr float kLaunchUs = 4.f;
+            constexpr float kLaunchUs = 6.f;        // set-up, first copies, end
             if (first.splits == 1 && first.us + rest.us + kLaunchUs < whole.us) {
                 const dropit_status s = input_grad_rows(first, from, w, rows, C, H, to, dev_status, stream);
                 return s == DROPIT_OK ? input_grad_rows(rest, from + rows * 2 * H, w, M - rows, C, H, to + rows * C, dev_status, stream) : s;
