@@ -568,21 +568,20 @@ static dropit_status input_grad_rows(const Plan& p, const uint16_t* dgu, const v
     return launch(kInputGrad, kernel_of(kInputGrad, p.width, DROPIT_GATE_SILU), p, maps, s, dev_status, stream);
 }
 
-// A last wave that few pairs take part in costs as much as a full one (12608 x 4096 -> 768: 150 tiles on 74 pairs, 73 us).  Where it pays, the rows of the
-// full waves are one launch and the rest, with a plan of its own, another.
+// A last wave of a few tiles takes as long as their whole summed axis.  Where it is a sixteenth of the pairs or less, the rows of the full waves are one
+// launch and the rest, whose pairs share the axis, another: 12608 x 4096 -> 768 (150 tiles on 74 pairs) 66 us, in one launch 69.5.  With more tiles in
+// the last wave a second launch costs more than it saves (32768 rows, 14 tiles: 154 and 151 us; 25000 x 2048 -> 384, 48 tiles: 61 and 53).
 dropit_status gated_tc_input_grad(const void* dgu, const void* w, int64_t M, int64_t C, int64_t H, void* dx, int32_t* dev_status, cudaStream_t stream) {
     const Plan whole = plan(kInputGrad, M, C, 2 * H);
     const uint16_t* from = reinterpret_cast<const uint16_t*>(dgu);
     uint16_t* to = reinterpret_cast<uint16_t*>(dx);
-    if (whole.splits == 1 && whole.tiles > whole.clusters) {
-        const int64_t rows = (int64_t)kRows * (whole.tiles / whole.clusters * whole.clusters / whole.tiles_n);
+    const int last = whole.tiles % whole.clusters;
+    if (whole.splits == 1 && whole.tiles > whole.clusters && last && 16 * last <= whole.clusters) {
+        const int64_t rows = (int64_t)kRows * ((whole.tiles - last) / whole.tiles_n);
         if (rows > 0 && rows < M) {
-            const Plan first = plan(kInputGrad, rows, C, 2 * H), rest = plan(kInputGrad, M - rows, C, 2 * H);
-            constexpr float kLaunchUs = 6.f;        // set-up, first copies, end
-            if (first.splits == 1 && first.us + rest.us + kLaunchUs < whole.us) {
-                const dropit_status s = input_grad_rows(first, from, w, rows, C, H, to, dev_status, stream);
-                return s == DROPIT_OK ? input_grad_rows(rest, from + rows * 2 * H, w, M - rows, C, H, to + rows * C, dev_status, stream) : s;
-            }
+            const dropit_status s = input_grad_rows(plan(kInputGrad, rows, C, 2 * H), from, w, rows, C, H, to, dev_status, stream);
+            if (s != DROPIT_OK) return s;
+            return input_grad_rows(plan(kInputGrad, M - rows, C, 2 * H), from + rows * 2 * H, w, M - rows, C, H, to + rows * C, dev_status, stream);
         }
     }
     return input_grad_rows(whole, from, w, M, C, H, to, dev_status, stream);
