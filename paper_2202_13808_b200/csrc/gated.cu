@@ -24,7 +24,8 @@ __device__ __forceinline__ void put(float* p, float v) { *p = v; }
 // four groups of 64 threads share out the summed axis, 16 of every 64 values each, 4 x 4 outputs a thread (two of them in the forward pass: the
 // gate's and the other), and add up in order at the end.  The next 64 values are on their way while these are multiplied.
 // A tile lies as [k][32] with its quads of outputs exchanged by k mod 8: conflict-free both for the transposing stores and for the reads.
-// fp32 197 x 387 -> 771 and back: forward 14 us, dx 20 (64 x 64 tiles without groups: 87 and 265).
+// Up to four CTAs of a cluster share out the summed axis too, where that evens out the SMs; the first one adds what the others send.
+// fp32 197 x 387 -> 771 and back: forward 23 us, dx 17 (one CTA a tile: 24 and 36; 64 x 64 tiles without groups: 87 and 265).
 // ---------------------------------------------------------------------------------------------
 constexpr int kTile = 32, kStep = 64, kFmaThreads = 256, kGroups = 4;
 struct __align__(16) FmaTile {
@@ -33,15 +34,13 @@ struct __align__(16) FmaTile {
     __device__ float4 quad(int k, int q) const { return *reinterpret_cast<const float4*>(&v[k][(q ^ (k & 7)) * 4]); }
 };
 
-// kStep values of 32 rows of a row-major matrix [rows x K] from (row0, k0): 8 values x 4 rows a warp and load
+// kStep values of 32 rows of a row-major matrix [rows x K] from (row0, k0): 8 values x 4 rows a warp and load.  (All matrices have fewer than 2^31 values.)
 template <typename T>
-__device__ __forceinline__ void fetch_rows(float (&r)[8], const T* a, int64_t row0, int64_t rows, int64_t k0, int64_t K) {
-    const int64_t k = k0 + (threadIdx.x >> 5) * 8 + (threadIdx.x & 7);
+__device__ __forceinline__ void fetch_rows(float (&r)[8], const T* a, uint32_t row0, uint32_t rows, uint32_t k0, uint32_t K) {
+    const uint32_t k = k0 + (threadIdx.x >> 5) * 8 + (threadIdx.x & 7), row = row0 + ((threadIdx.x >> 3) & 3);
+    const uint32_t there = k < K && row < rows ? min((rows - row + 3) / 4, 8u) : 0u, at = row * K + k;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const int64_t row = row0 + ((threadIdx.x >> 3) & 3) + 4 * j;
-        r[j] = k < K && row < rows ? to_float(a[row * K + k]) : 0.f;
-    }
+    for (uint32_t j = 0; j < 8; ++j) r[j] = j < there ? to_float(a[at + 4 * j * K]) : 0.f;
 }
 __device__ __forceinline__ void stage_rows(FmaTile& t, const float (&r)[8]) {
 #pragma unroll
@@ -49,13 +48,11 @@ __device__ __forceinline__ void stage_rows(FmaTile& t, const float (&r)[8]) {
 }
 // kStep rows x 32 columns of a row-major matrix [K x cols]
 template <typename T>
-__device__ __forceinline__ void fetch_cols(float (&r)[8], const T* b, int64_t k0, int64_t K, int64_t col0, int64_t cols) {
-    const int64_t c = col0 + (threadIdx.x & 31);
+__device__ __forceinline__ void fetch_cols(float (&r)[8], const T* b, uint32_t k0, uint32_t K, uint32_t col0, uint32_t cols) {
+    const uint32_t c = col0 + (threadIdx.x & 31), k = k0 + (threadIdx.x >> 5);
+    const uint32_t there = c < cols && k < K ? min((K - k + 7) / 8, 8u) : 0u, at = k * cols + c;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const int64_t k = k0 + (threadIdx.x >> 5) + 8 * j;
-        r[j] = k < K && c < cols ? to_float(b[k * cols + c]) : 0.f;
-    }
+    for (uint32_t j = 0; j < 8; ++j) r[j] = j < there ? to_float(b[at + 8 * j * cols]) : 0.f;
 }
 __device__ __forceinline__ void stage_cols(FmaTile& t, const float (&r)[8]) {
 #pragma unroll
@@ -85,27 +82,58 @@ __device__ __forceinline__ void join(float (&out)[4], const float (&acc)[4][4], 
     }
 }
 
+// The part of the summed axis that a CTA of a cluster takes, in whole steps.
+__device__ __forceinline__ void my_part(uint32_t K, uint32_t& begin, uint32_t& end) {
+    const uint32_t steps = (K + kStep - 1) / kStep;
+    begin = steps * blockIdx.z / gridDim.z * kStep;
+    end = min(K, steps * (blockIdx.z + 1) / gridDim.z * kStep);
+}
+// Sums of the cluster's CTAs in the first one, added in order; false in the others.  room: of every CTA, kCluster - 1 times N tiles.
+constexpr int kMaxCluster = 4;
+template <int N>
+__device__ __forceinline__ bool gather(float (&sums)[N][4], float* room) {
+    if (gridDim.z == 1) return true;
+    ptx::cluster_sync_all();             // the room is free in all of them
+    if (blockIdx.z) {
+        const uint32_t to = ptx::map_shared_to_cta(ptx::smem_u32(room + (blockIdx.z - 1) * N * kTile * kTile + threadIdx.x), 0);
+#pragma unroll
+        for (int t = 0; t < N; ++t)
+#pragma unroll
+            for (int n = 0; n < 4; ++n) ptx::st_cluster_u32(to + (t * kTile * kTile + n * kFmaThreads) * 4, __float_as_uint(sums[t][n]));
+    }
+    ptx::cluster_sync_all();
+    if (blockIdx.z) return false;
+    for (int r = 0; r < (int)gridDim.z - 1; ++r)
+#pragma unroll
+        for (int t = 0; t < N; ++t)
+#pragma unroll
+            for (int n = 0; n < 4; ++n) sums[t][n] += room[(r * N + t) * kTile * kTile + n * kFmaThreads + threadIdx.x];
+    return true;
+}
+
 template <typename T, int GATE>
-__global__ void __launch_bounds__(kFmaThreads)
-gated_fma_kernel(const T* __restrict__ x, const T* __restrict__ w, const T* __restrict__ bias, int64_t M, int64_t C, int64_t H, T* __restrict__ h,
+__global__ void __launch_bounds__(kFmaThreads, 2)
+gated_fma_kernel(const T* __restrict__ x, const T* __restrict__ w, const T* __restrict__ bias, uint32_t M, uint32_t C, uint32_t H, T* __restrict__ h,
                  T* __restrict__ gu) {
     __shared__ FmaTile tiles[3];
-    const int64_t row0 = (int64_t)blockIdx.x * kTile, col0 = (int64_t)blockIdx.y * kTile;
+    const uint32_t row0 = blockIdx.x * kTile, col0 = blockIdx.y * kTile;
     const int group = threadIdx.x / 64, ty = (threadIdx.x / 8) % 8, tx = threadIdx.x % 8;
     float g[4][4] = {}, u[4][4] = {}, ra[8], rg[8], ru[8];
-    fetch_rows(ra, x, row0, M, 0, C);
-    fetch_rows(rg, w, col0, H, 0, C);
-    fetch_rows(ru, w + H * C, col0, H, 0, C);
-    for (int64_t k0 = 0; k0 < C; k0 += kStep) {
+    uint32_t begin, end;
+    my_part(C, begin, end);
+    fetch_rows(ra, x, row0, M, begin, C);
+    fetch_rows(rg, w, col0, H, begin, C);
+    fetch_rows(ru, w + (size_t)H * C, col0, H, begin, C);
+    for (uint32_t k0 = begin; k0 < end; k0 += kStep) {
         __syncthreads();
         stage_rows(tiles[0], ra);
         stage_rows(tiles[1], rg);
         stage_rows(tiles[2], ru);
         __syncthreads();
-        if (k0 + kStep < C) {
+        if (k0 + kStep < end) {
             fetch_rows(ra, x, row0, M, k0 + kStep, C);
             fetch_rows(rg, w, col0, H, k0 + kStep, C);
-            fetch_rows(ru, w + H * C, col0, H, k0 + kStep, C);
+            fetch_rows(ru, w + (size_t)H * C, col0, H, k0 + kStep, C);
         }
 #pragma unroll 8
         for (int i = 0; i < kStep / kGroups; ++i) {
@@ -115,14 +143,15 @@ gated_fma_kernel(const T* __restrict__ x, const T* __restrict__ w, const T* __re
             multiply(u, p, tiles[2].quad(k, tx));
         }
     }
-    float gs[4], us[4];
-    join(gs, g, &tiles[0].v[0][0]);
-    join(us, u, &tiles[0].v[0][0]);
+    float sums[2][4];
+    join(sums[0], g, &tiles[0].v[0][0]);
+    join(sums[1], u, &tiles[0].v[0][0]);
+    if (!gather(sums, &tiles[0].v[0][0])) return;
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
-        const int64_t r = row0 + (n * kFmaThreads + threadIdx.x) / kTile, c = col0 + threadIdx.x % kTile;
+        const size_t r = row0 + (n * kFmaThreads + threadIdx.x) / kTile, c = col0 + threadIdx.x % kTile;
         if (r >= M || c >= H) continue;
-        const float gv = gs[n] + (bias ? to_float(bias[c]) : 0.f), uv = us[n] + (bias ? to_float(bias[H + c]) : 0.f);
+        const float gv = sums[0][n] + (bias ? to_float(bias[c]) : 0.f), uv = sums[1][n] + (bias ? to_float(bias[H + c]) : 0.f);
         put(h + r * H + c, gate_value<GATE, false>(gv) * uv);
         if (gu) {
             put(gu + r * 2 * H + c, gv);
@@ -132,20 +161,22 @@ gated_fma_kernel(const T* __restrict__ x, const T* __restrict__ w, const T* __re
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kFmaThreads)
-input_grad_fma_kernel(const T* __restrict__ dgu, const T* __restrict__ w, int64_t M, int64_t C, int64_t K, T* __restrict__ dx) {
+__global__ void __launch_bounds__(kFmaThreads, 2)
+input_grad_fma_kernel(const T* __restrict__ dgu, const T* __restrict__ w, uint32_t M, uint32_t C, uint32_t K, T* __restrict__ dx) {
     __shared__ FmaTile tiles[2];
-    const int64_t row0 = (int64_t)blockIdx.x * kTile, col0 = (int64_t)blockIdx.y * kTile;
+    const uint32_t row0 = blockIdx.x * kTile, col0 = blockIdx.y * kTile;
     const int group = threadIdx.x / 64, ty = (threadIdx.x / 8) % 8, tx = threadIdx.x % 8;
     float acc[4][4] = {}, ra[8], rb[8];
-    fetch_rows(ra, dgu, row0, M, 0, K);
-    fetch_cols(rb, w, 0, K, col0, C);
-    for (int64_t k0 = 0; k0 < K; k0 += kStep) {
+    uint32_t begin, end;
+    my_part(K, begin, end);
+    fetch_rows(ra, dgu, row0, M, begin, K);
+    fetch_cols(rb, w, begin, K, col0, C);
+    for (uint32_t k0 = begin; k0 < end; k0 += kStep) {
         __syncthreads();
         stage_rows(tiles[0], ra);
         stage_cols(tiles[1], rb);
         __syncthreads();
-        if (k0 + kStep < K) {
+        if (k0 + kStep < end) {
             fetch_rows(ra, dgu, row0, M, k0 + kStep, K);
             fetch_cols(rb, w, k0 + kStep, K, col0, C);
         }
@@ -155,12 +186,13 @@ input_grad_fma_kernel(const T* __restrict__ dgu, const T* __restrict__ w, int64_
             multiply(acc, tiles[0].quad(k, ty), tiles[1].quad(k, tx));
         }
     }
-    float s[4];
-    join(s, acc, &tiles[0].v[0][0]);
+    float sums[1][4];
+    join(sums[0], acc, &tiles[0].v[0][0]);
+    if (!gather(sums, &tiles[0].v[0][0])) return;
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
-        const int64_t r = row0 + (n * kFmaThreads + threadIdx.x) / kTile, c = col0 + threadIdx.x % kTile;
-        if (r < M && c < C) put(dx + r * C + c, s[n]);
+        const size_t r = row0 + (n * kFmaThreads + threadIdx.x) / kTile, c = col0 + threadIdx.x % kTile;
+        if (r < M && c < C) put(dx + r * C + c, sums[0][n]);
     }
 }
 
@@ -384,12 +416,37 @@ dropit_status launch_backward(const void* dh, const void* gu, int64_t M, int64_t
     return check_launch();
 }
 
+// Tiles of 32 rows x 32 columns, and for each as many CTAs as have the fullest SM do the fewest steps of the summed axis (joining costs about one).
+template <typename... Params, typename... Args>
+dropit_status launch_fma(void (*kernel)(Params...), int64_t rows, int64_t cols, int64_t K, cudaStream_t stream, Args... args) {
+    const int64_t tiles = ((rows + kTile - 1) / kTile) * ((cols + kTile - 1) / kTile), steps = (K + kStep - 1) / kStep;
+    unsigned parts = 1;
+    int64_t least = 0;
+    for (unsigned p = 1; p <= kMaxCluster && p <= steps; ++p) {
+        const int64_t rounds = (tiles * p + sm_count() - 1) / sm_count(), time = rounds * ((steps + p - 1) / p) + (p > 1 ? 1 : 0);
+        if (p == 1 || time < least) parts = p, least = time;
+    }
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = parts;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((rows + kTile - 1) / kTile), (unsigned)((cols + kTile - 1) / kTile), parts);
+    cfg.blockDim = dim3(kFmaThreads);
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return DROPIT_ERR_CUDA;
+    }
+    return check_launch();
+}
 template <typename T>
-void launch_fma(const void* x, const void* w, const void* bias, int64_t M, int64_t C, int64_t H, dropit_gate gate, void* h, void* gu, cudaStream_t stream) {
-    const dim3 grid((unsigned)((M + kTile - 1) / kTile), (unsigned)((H + kTile - 1) / kTile));
+dropit_status gated_fma(const void* x, const void* w, const void* bias, int64_t M, int64_t C, int64_t H, dropit_gate gate, void* h, void* gu, cudaStream_t stream) {
     auto kernel = gate == DROPIT_GATE_SILU ? gated_fma_kernel<T, DROPIT_GATE_SILU>
                   : gate == DROPIT_GATE_GELU ? gated_fma_kernel<T, DROPIT_GATE_GELU> : gated_fma_kernel<T, DROPIT_GATE_RELU>;
-    kernel<<<grid, kFmaThreads, 0, stream>>>((const T*)x, (const T*)w, (const T*)bias, M, C, H, (T*)h, (T*)gu);
+    return launch_fma(kernel, M, H, C, stream, (const T*)x, (const T*)w, (const T*)bias, M, C, H, (T*)h, (T*)gu);
 }
 
 bool gate_ok(dropit_gate g) { return g == DROPIT_GATE_SILU || g == DROPIT_GATE_GELU || g == DROPIT_GATE_RELU; }
@@ -450,9 +507,8 @@ extern "C" dropit_status dropit_gated_linear(const void* x, const void* w, const
             x, w, bias, (int)M, (int)C, (int)H, h, gu, as_stream(cuda_stream));
     if (dtype == DROPIT_BF16 && gated_tc_takes(M, C, H)) return gated_tc_forward(x, w, bias, M, C, H, gate, h, gu, dev_status, as_stream(cuda_stream));
     if (H > (int64_t)65535 * kTile) return DROPIT_ERR_UNSUPPORTED;
-    if (dtype == DROPIT_BF16) launch_fma<uint16_t>(x, w, bias, M, C, H, gate, h, gu, as_stream(cuda_stream));
-    else launch_fma<float>(x, w, bias, M, C, H, gate, h, gu, as_stream(cuda_stream));
-    return check_launch();
+    return dtype == DROPIT_BF16 ? gated_fma<uint16_t>(x, w, bias, M, C, H, gate, h, gu, as_stream(cuda_stream))
+                                : gated_fma<float>(x, w, bias, M, C, H, gate, h, gu, as_stream(cuda_stream));
 }
 
 extern "C" dropit_status dropit_gated_linear_backward_workspace(int64_t M, int64_t H, dropit_dtype dtype, size_t* workspace_bytes) {
@@ -481,10 +537,7 @@ extern "C" dropit_status dropit_gated_input_grad(const void* dgu, const void* w,
     if (!buffers_ok({dgu, w, dx})) return DROPIT_ERR_INVALID_ARG;
     if (dtype == DROPIT_BF16 && gated_tc_takes(M, C, H)) return gated_tc_input_grad(dgu, w, M, C, H, dx, dev_status, as_stream(cuda_stream));
     if (C > (int64_t)65535 * kTile) return DROPIT_ERR_UNSUPPORTED;
-    const dim3 grid((unsigned)((M + kTile - 1) / kTile), (unsigned)((C + kTile - 1) / kTile));
-    if (dtype == DROPIT_BF16)
-        input_grad_fma_kernel<uint16_t><<<grid, kFmaThreads, 0, as_stream(cuda_stream)>>>((const uint16_t*)dgu, (const uint16_t*)w, M, C, 2 * H, (uint16_t*)dx);
-    else
-        input_grad_fma_kernel<float><<<grid, kFmaThreads, 0, as_stream(cuda_stream)>>>((const float*)dgu, (const float*)w, M, C, 2 * H, (float*)dx);
-    return check_launch();
+    cudaStream_t stream = as_stream(cuda_stream);
+    return dtype == DROPIT_BF16 ? launch_fma(input_grad_fma_kernel<uint16_t>, M, C, 2 * H, stream, (const uint16_t*)dgu, (const uint16_t*)w, M, C, 2 * H, (uint16_t*)dx)
+                                : launch_fma(input_grad_fma_kernel<float>, M, C, 2 * H, stream, (const float*)dgu, (const float*)w, M, C, 2 * H, (float*)dx);
 }
