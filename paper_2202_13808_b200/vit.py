@@ -26,14 +26,15 @@ from .nn import DropITGatedLinear, DropITGeluLinear, DropITRotary, convert_linea
 from .optim import DropITAdamW
 
 
-class StockGatedLinear(nn.Linear):
+class StockGatedLinear(nn.Module):
     """silu(x Wg^T + bg) * (x Wu^T + bu) in stock operations: what DropITGatedLinear is compared with, and takes its parameters from."""
 
     def __init__(self, in_features: int, hidden_features: int, **kw):
-        super().__init__(in_features, 2 * hidden_features, **kw)
+        super().__init__()
+        self.both = nn.Linear(in_features, 2 * hidden_features, **kw)
 
     def forward(self, x):
-        a, u = super().forward(x).chunk(2, -1)
+        a, u = self.both(x).chunk(2, -1)
         return F.silu(a) * u
 
 
@@ -108,7 +109,7 @@ def build_vit_b16(gamma=None, device="cuda", dtype=torch.bfloat16, depth=12, see
     if gamma is not None:
         for b in model.blocks:
             if b.gated:
-                old = b.fc1
+                old = b.fc1.both
                 b.fc1 = DropITGatedLinear(old.in_features, old.out_features // 2, gamma=gamma, device=old.weight.device, dtype=old.weight.dtype)
                 b.fc1.weight, b.fc1.bias = old.weight, old.bias
         if fuse_gelu and ffn == "gelu":

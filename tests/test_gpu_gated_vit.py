@@ -41,7 +41,7 @@ def test_gradients_of_a_block_against_64_bits(cuda_device):
     block = vit.Block(60, 3, 96, "gated", True).to(cuda_device)
     want = copy.deepcopy(block).double()
     want.rotary = _Turn(block.rotary)
-    old = block.fc1
+    old = block.fc1.both
     block.fc1 = DropITGatedLinear(60, 64, gamma=0.0, device=cuda_device)
     block.fc1.weight, block.fc1.bias = old.weight, old.bias
     convert_linear_layers(block, 0.0)
@@ -53,7 +53,8 @@ def test_gradients_of_a_block_against_64_bits(cuda_device):
     out, ref = block(x, grid), want(y, grid)
     out.backward(g)
     ref.backward(g.double())
-    pairs = [(out, ref), (x.grad, y.grad)] + [(p.grad, dict(want.named_parameters())[n].grad) for n, p in block.named_parameters()]
+    theirs = {n.replace("fc1.both.", "fc1."): p.grad for n, p in want.named_parameters()}
+    pairs = [(out, ref), (x.grad, y.grad)] + [(p.grad, theirs[n]) for n, p in block.named_parameters()]
     assert len(pairs) == 2 + 12
     for a, b in pairs:
         assert float((a.double() - b).abs().max()) <= 1e-4 * float(b.abs().max())
@@ -89,7 +90,7 @@ def test_a_step_captured_whole(cuda_device):
     def make():
         torch.manual_seed(0)
         model = vit.ViT(image=32, patch=8, dim=64, depth=1, heads=2, mlp=96, classes=10, ffn="gated", positions="rotary").to(cuda_device)
-        old = model.blocks[0].fc1
+        old = model.blocks[0].fc1.both
         model.blocks[0].fc1 = DropITGatedLinear(64, 64, gamma=0.5, device=cuda_device)
         model.blocks[0].fc1.weight, model.blocks[0].fc1.bias = old.weight, old.bias
         return model, dropit.DropITAdamW(model.parameters(), lr=1e-3, state_bits=8)
@@ -142,3 +143,52 @@ def test_what_the_options_refuse(cuda_device):
         vit.ViT(positions="none")
     with pytest.raises(ValueError):
         vit.make_optimizer(nn.Linear(2, 2), "lion", 1e-3)
+
+
+def test_converting_the_stock_gated_block_keeps_its_gate(cuda_device):
+    torch.manual_seed(3)
+    block = vit.Block(64, 2, 96, "gated").to(cuda_device)
+    x = torch.randn(2, 5, 64, device=cuda_device)
+    want = block(x)
+    convert_linear_layers(block, 0.0)
+    got = block(x)
+    assert float((got - want).detach().abs().max()) <= 1e-4 * float(want.detach().abs().max())
+
+
+def test_layers_of_two_streams_at_once(cuda_device):
+    """Two streams run the layer, the rotation and a step of their own at the same time: each gets what it gets alone."""
+    def work(seed):
+        g = torch.Generator(device=cuda_device).manual_seed(seed)
+        torch.manual_seed(seed)
+        layer = DropITGatedLinear(256, 384, gamma=0.8, device=cuda_device, dtype=torch.bfloat16).train()
+        opt = dropit.DropITAdamW(layer.parameters(), lr=1e-2, state_bits=8, dither=True)
+        rot = dropit.DropITRotary(64, (32, 32))
+        x = torch.randn(2100, 256, generator=g, device=cuda_device).bfloat16().requires_grad_(True)
+        dh = torch.randn(2100, 384, generator=g, device=cuda_device).bfloat16()
+        at = torch.randint(0, 99, (2100, 2), generator=g, device=cuda_device)
+
+        def once():
+            x.grad = None
+            opt.zero_grad()
+            h = layer(x)
+            h.backward(dh)
+            opt.step()
+            return [h.detach(), x.grad, rot(h.detach().view(2100, 6, 64), None, at)[0]] + [p.detach().clone() for p in layer.parameters()]
+        return once
+    alone = []
+    for seed in (1, 2):
+        once = work(seed)
+        alone.append([once() for _ in range(4)])
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    together = [work(1), work(2)]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(4):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(together[i]())
+    torch.cuda.synchronize()
+    dropit.check_device_status(cuda_device)
+    for a, b in zip(alone, got):
+        for one, other in zip(a, b):
+            assert all(torch.equal(p, q) for p, q in zip(one, other))
