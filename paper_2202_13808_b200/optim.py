@@ -54,6 +54,8 @@ class DropITAdamW(torch.optim.Optimizer):
         lr = group["lr"]
         if not isinstance(lr, torch.Tensor) and not lr >= 0:
             raise ValueError("lr must not be negative, got %r" % (lr,))
+        if len({id(p) for p in group["params"]}) != len(group["params"]):
+            raise ValueError("a parameter is given twice")
         for p in group["params"]:
             if p.dtype not in (torch.bfloat16, torch.float32):
                 raise TypeError("parameters are bf16 or fp32, got %s" % p.dtype)
@@ -95,6 +97,9 @@ class DropITAdamW(torch.optim.Optimizer):
         device = params[0].device
         if any(p.device != device for p in params) or device.type != "cuda":
             raise ValueError("all parameters must be on one CUDA device (there is no CPU path)")
+        spans = sorted((p.data_ptr(), p.data_ptr() + p.numel() * p.element_size()) for p in params if p.numel())
+        if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
+            raise ValueError("two parameters share memory: one step would take it in turns with itself")
         before = {id(p): self.state[p] for p in params if self.state.get(p)}
         first, total = [], 0
         for p in params:

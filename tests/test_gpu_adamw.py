@@ -292,6 +292,11 @@ def test_refusals(cuda_device):
         cpu = torch.nn.Parameter(torch.ones(3))
         cpu.grad = torch.ones(3)
         dropit.DropITAdamW([cpu]).step()
+    with pytest.raises(ValueError):
+        dropit.DropITAdamW([p, p])
+    both = torch.ones(12, device="cuda")
+    with pytest.raises(ValueError, match="share memory"):
+        dropit.DropITAdamW([torch.nn.Parameter(both[:8]), torch.nn.Parameter(both[4:])]).init_state()
     opt = make()
     p.grad = torch.ones_like(p)
     for bad in (1.0, torch.ones(1), torch.ones(1, device="cuda").half(), torch.ones(2, device="cuda")):
@@ -333,3 +338,36 @@ def test_hooks_and_closures(cuda_device):
     version = p._version
     opt.step()
     assert p._version == version + 1        # autograd sees that p has changed
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_tensors_of_many_runs(cuda_device, dtype):
+    """Enough values that warps take whole runs of blocks, with a ragged end and small tensors around; a second step on the first one's state."""
+    g = torch.Generator(device="cuda").manual_seed(6)
+    sizes = [300, 27_000_037, 5, 4096 * 3 + 1]
+    params = [torch.nn.Parameter((torch.randn(n, generator=g, device="cuda") * 0.1).to(dtype)) for n in sizes]
+    opt = dropit.DropITAdamW(params, lr=1e-2, weight_decay=0.1, state_bits=8, seed=9)
+    for t in (1, 2):
+        before = []
+        for p in params:
+            p.grad = (torch.randn(p.shape, generator=g, device="cuda") * 0.02).to(dtype)
+            s = opt.init_state(p)
+            block = torch.arange(p.numel(), device="cuda") // BLOCK
+            before.append((p.detach().double().clone(), s["exp_avg"].double() * s["exp_avg_scale"].double()[block],
+                           (s["exp_avg_root"].double() * s["exp_avg_root_scale"].double()[block]) ** 2, block))
+        opt.step()
+        for p, (p0, m0, v0, block) in zip(params, before):
+            s = opt.state[p]
+            want, m, v, bound = _step64(p0, p.grad.double(), m0, v0, t, 1e-2, 0.1, 0.9, 0.999, 1e-8)
+            if dtype == torch.bfloat16:
+                bound = 2 * bound + 2.0 ** -8 * want.abs()
+            assert bool(((p.detach().double() - want).abs() <= bound).all()) and int(s["step"]) == t
+            # m in fp32 is off by e = 6 units (2^-24) of its terms' size (see _step64), a root by a part in 1e5 at most
+            e = 6 * 2.0 ** -24 * (0.9 * m0.abs() + 0.1 * p.grad.double().abs())
+            for x, off, codes, scale in ((m, e, s["exp_avg"], s["exp_avg_scale"]), (v.sqrt(), 0 * e, s["exp_avg_root"], s["exp_avg_root_scale"])):
+                top = torch.nn.functional.pad(x, (0, -x.numel() % BLOCK)).view(-1, BLOCK).abs().amax(1)
+                assert bool(((scale.double() - top / 448).abs() <= 1e-6 * top / 448).all())
+                # Within a code's spacing: an eighth of the value, 2^-9 of the scale at least.  What is coded is x' with |x' - x| <= e, and
+                # |held - x| <= spacing(x') + e <= spacing(x) + e / 8 + e: where bf16 gradients cancel 0.9 m exactly, x and x' lie on both sides of zero.
+                held, unit = codes.double() * scale.double()[block], scale.double()[block]
+                assert bool(((held - x).abs() <= torch.maximum(x.abs() / 8, unit * 2.0 ** -9) * (1 + 1e-5) + off * 9 / 8).all())
