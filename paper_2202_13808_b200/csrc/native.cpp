@@ -10,6 +10,7 @@
 #include <torch/extension.h>
 #include <ATen/MemoryOverlap.h>
 
+#include <cstdlib>
 #include <mutex>
 #include <tuple>
 #include <vector>
@@ -475,6 +476,15 @@ dropit_rotary_tensor rotary_tensor(const Tensor& in, Tensor& out, const dropit_r
 }
 Tensor rotary_input(const Tensor& t) { return t.dim() && t.stride(-1) != 1 ? t.contiguous() : t; }
 
+// Whether slices along the heads of one projection have channels in common.
+bool share_channels(const Tensor& q, const Tensor& k) {
+    if (q.numel() == 0 || k.numel() == 0 || q.dim() < 3 || k.dim() != q.dim() || !q.storage().is_alias_of(k.storage())) return false;
+    const int64_t off = k.storage_offset() - q.storage_offset();
+    for (int64_t h = 1 - k.size(-2); h < q.size(-2); ++h)          // heads of q less heads of k
+        if (std::abs(off - h * q.stride(-2)) < q.size(-1)) return true;
+    return false;
+}
+
 std::tuple<Tensor, c10::optional<Tensor>> rotary(const Tensor& q_in, const c10::optional<Tensor>& k_in, const Tensor& positions, const Tensor& plan_bytes,
                                                  bool inverse, bool in_place) {
     const dropit_rotary_plan* plan = plan_of(plan_bytes);
@@ -485,6 +495,7 @@ std::tuple<Tensor, c10::optional<Tensor>> rotary(const Tensor& q_in, const c10::
         throw py::value_error("in place: the channels of a head must lie together");
     if (in_place && (at::has_internal_overlap(q_in) == at::MemOverlap::Yes || (has_k && at::has_internal_overlap(*k_in) == at::MemOverlap::Yes)))
         throw py::value_error("in place: an expanded tensor has no place of its own");
+    if (in_place && has_k && share_channels(q_in, *k_in)) throw py::value_error("in place: q and k share values");
     const Tensor q = rotary_input(q_in), k = has_k ? rotary_input(*k_in) : Tensor();
     c10::cuda::CUDAGuard guard(q.device());
     Tensor q_out = in_place ? q : Tensor(at::detail::empty_cuda(q.sizes(), q.scalar_type(), q.device(), c10::nullopt)), k_out;

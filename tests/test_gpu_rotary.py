@@ -49,9 +49,10 @@ def _check(got, x, positions, sections, theta, interleaved, shared, sign=1.0):
 
 
 # batch, length, query and key heads, head_dim, sections: whole vectors of 8 and of 4, odd numbers of pairs, heads that are rotated in part, one axis,
-# an axis without channels, one token and many.
+# an axis without channels, one token and many; more heads than are looked up at once, more units in a head than threads in a block, tiny heads.
 SHAPES = [(2, 197, 12, 12, 64, (32, 32)), (1, 1, 16, 4, 128, (48, 40, 40)), (3, 37, 3, 1, 40, (20, 20)), (2, 19, 2, 2, 34, (10, 12, 6)),
-          (1, 1000, 5, 3, 96, (32, 0, 32)), (5, 7, 1, 1, 2, (2,)), (1, 3, 2, 1, 512, (256, 256)), (4, 50, 6, 2, 72, (24, 24, 16, 8))]
+          (1, 1000, 5, 3, 96, (32, 0, 32)), (5, 7, 1, 1, 2, (2,)), (1, 3, 2, 1, 512, (256, 256)), (4, 50, 6, 2, 72, (24, 24, 16, 8)),
+          (1, 3, 1100, 7, 16, (16,)), (2, 2, 2, 1, 4096, (256, 256)), (3, 90, 1, 1, 16, (8, 8))]
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
@@ -204,6 +205,13 @@ def test_refusals(cuda_device):
             dropit.dropit_rotary(q, k, positions, plan)
     with pytest.raises(ValueError):
         dropit.dropit_rotary(x, x, p, plan[:-1])
+    both = torch.zeros(1, 4, 4, 16, device=cuda_device)
+    for q, k in ((x, x), (both[:, :, :3], both[:, :, 2:])):
+        with pytest.raises(ValueError, match="share"):
+            dropit.dropit_rotary(q, k, p, plan, in_place=True)
+    dropit.dropit_rotary(both[:, :, :2], both[:, :, 2:], p, plan, in_place=True)
+    dropit.dropit_rotary(both[:, :, :1], both[:, :, 1:], p, plan, in_place=True)
+    dropit.dropit_rotary(both[:, :, 3:], both[:, :, :3], p, plan, in_place=True)
 
 
 def test_a_token_far_into_a_batch_of_more_than_two_to_the_31_values(cuda_device):
