@@ -282,7 +282,8 @@ dropit_status launch_few(const void* x, const void* w, const void* bias, int M, 
 // ---------------------------------------------------------------------------------------------
 // dgu = dh u f'(a) | dh f(a), and their column sums.  A warp walks down a strip of 32 * VEC columns, so that every thread keeps the sums of
 // its columns; a block's eight warps meet in shared memory, the blocks of a strip in `partial` [chunks x 2H].
-// Bound by HBM: three values read and two written for every two sums.
+// Bound by HBM: three values read and two written for every two sums (12608 x 2048 in bf16: 258 MB in 42 us).  dgu in bf16 is rounded once, as the products
+// take it; the column sums are of what is not rounded yet.
 // ---------------------------------------------------------------------------------------------
 constexpr int kBackThreads = 256, kBackWarps = kBackThreads / 32;
 
