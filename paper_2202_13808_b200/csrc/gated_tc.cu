@@ -98,13 +98,16 @@ __device__ __forceinline__ void store_square(uint16_t* to, size_t pitch, uint8_t
     }
     __syncwarp();
 }
-// acc += 32 values of the bias from column c on (limit: its end)
-__device__ __forceinline__ void add_bias(float (&acc)[32], const uint16_t* bias, int c, int limit) {
+// 32 values of the bias from column c on (limit, a multiple of 8 and at least that: its end; behind it anything).  All loads go out at once, in front of the
+// accumulator's: one after the other 12608 x 768 -> 2048 with a and u took 80 us instead of 74, 591 rows 16.6 instead of 15.8.
+__device__ __forceinline__ void load_bias(uint4 (&q)[4], const uint16_t* bias, int c, int limit) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) q[e] = __ldg(reinterpret_cast<const uint4*>(bias + min(c + 8 * e, limit - 8)));
+}
+__device__ __forceinline__ void add_bias(float (&acc)[32], const uint4 (&q)[4]) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        if (c + 8 * e >= limit) break;
-        const uint4 q = __ldg(reinterpret_cast<const uint4*>(bias + c + 8 * e));
-        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+        const uint32_t w[4] = {q[e].x, q[e].y, q[e].z, q[e].w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             acc[8 * e + 2 * i] += __uint_as_float(w[i] << 16);
@@ -290,6 +293,11 @@ gated_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Shape
             for (int ch = half; ch < kChunks; ch += 2) {
                 const int c = ch * 32;
                 float v[32], u[MODE == kForward ? 32 : 1];
+                uint4 bias_v[4], bias_u[4];
+                if (MODE == kForward && shape.bias) {
+                    load_bias(bias_v, shape.bias, n0 + c, shape.N);
+                    load_bias(bias_u, shape.bias + shape.N, n0 + c, shape.N);
+                }
                 {
                     uint32_t r[32];
                     ptx::tmem_ld_32x32(tmem + c, r);
@@ -308,8 +316,8 @@ gated_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Shape
                 if (row >= shape.M || n0 + c >= shape.N) continue;
                 if constexpr (MODE == kForward) {
                     if (shape.bias) {
-                        add_bias(v, shape.bias, n0 + c, shape.N);
-                        add_bias(u, shape.bias + shape.N, n0 + c, shape.N);
+                        add_bias(v, bias_v);
+                        add_bias(u, bias_u);
                     }
                     if (shape.keep) {
                         store(&maps.out[1], v, n0 + c, row);
