@@ -241,6 +241,13 @@ Tensor gelu_linear(const Tensor& x, const Tensor& weight, const c10::optional<Te
     return GeluLinear::apply(x, weight, bias, gamma, fmt, table);
 }
 
+// The nodes below compute no forward-mode derivatives, and results without a tangent would pass for constants.
+bool has_tangent(const c10::optional<Tensor>& t) { return t.has_value() && t->defined() && t->_fw_grad(/*level=*/0).defined(); }
+void refuse_tangents(std::initializer_list<c10::optional<Tensor>> inputs, const char* name) {
+    for (const auto& t : inputs)
+        TORCH_CHECK_NOT_IMPLEMENTED(!has_tangent(t), name, " has no forward-mode derivative");
+}
+
 // ---- gated linear: h = f(x Wg^T + bg) * (x Wu^T + bu) ----
 
 // The library takes 16-byte aligned buffers; a slice may start anywhere.
@@ -258,6 +265,7 @@ struct GatedSizes {
     dropit_dtype dtype;
 };
 GatedSizes gated_sizes(const Tensor& x, const Tensor& weight, const c10::optional<Tensor>& bias) {
+    refuse_tangents({x, weight, bias}, "the gated linear");
     if (!x.is_cuda()) throw py::value_error("x must be a CUDA tensor (there is no CPU path)");
     GatedSizes s;
     s.dtype = dtype_code(x, "x");
@@ -304,6 +312,7 @@ std::tuple<Tensor, c10::optional<Tensor>> gated_linear(const Tensor& x, const Te
 }
 
 std::tuple<Tensor, c10::optional<Tensor>> gated_linear_backward(const Tensor& dh, const Tensor& gu, int64_t gate, bool want_db) {
+    refuse_tangents({dh, gu}, "the gated linear's gradient");
     if (!dh.is_cuda()) throw py::value_error("dh must be a CUDA tensor (there is no CPU path)");
     const dropit_dtype dt = dtype_code(dh, "dh");
     require_like(gu, dh, "gu", "dh");
@@ -327,6 +336,7 @@ std::tuple<Tensor, c10::optional<Tensor>> gated_linear_backward(const Tensor& dh
 }
 
 Tensor gated_input_grad(const Tensor& dgu, const Tensor& weight) {
+    refuse_tangents({dgu, weight}, "the gated linear's gradient");
     if (!dgu.is_cuda()) throw py::value_error("dgu must be a CUDA tensor (there is no CPU path)");
     const dropit_dtype dt = dtype_code(dgu, "dgu");
     require_like(weight, dgu, "weight", "dgu");
@@ -364,6 +374,7 @@ struct GatedLinearNode : public torch::autograd::Node {
         std::lock_guard<std::mutex> lock(mutex_);
         torch::autograd::variable_list out(3);
         if (!grads[0].defined()) return out;
+        refuse_tangents({grads[0]}, "the gated linear's gradient");
         const Tensor weight = weight_.unpack(), gu = gu_.unpack();          // an error, if they have been released
         const bool want_x = task_should_compute_output(0), want_w = task_should_compute_output(1), want_b = task_should_compute_output(2);
         {
@@ -487,6 +498,7 @@ bool share_channels(const Tensor& q, const Tensor& k) {
 
 std::tuple<Tensor, c10::optional<Tensor>> rotary(const Tensor& q_in, const c10::optional<Tensor>& k_in, const Tensor& positions, const Tensor& plan_bytes,
                                                  bool inverse, bool in_place) {
+    refuse_tangents({q_in, k_in, positions}, "the rotation");
     const dropit_rotary_plan* plan = plan_of(plan_bytes);
     if (!q_in.is_cuda()) throw py::value_error("q must be a CUDA tensor (there is no CPU path)");
     const dropit_dtype dt = dtype_code(q_in, "q");
@@ -661,6 +673,7 @@ PYBIND11_MODULE(_native, m) {
     m.def("weight_grad", torch::wrap_pybind_function_no_gil(weight_grad));
     m.def("conv_weight_grad", torch::wrap_pybind_function_no_gil(conv_weight_grad));
     m.def("gelu_linear", torch::wrap_pybind_function_no_gil(gelu_linear));
+    m.def("has_tangent", has_tangent);
     m.def("gated_linear", torch::wrap_pybind_function_no_gil(gated_linear));
     m.def("gated_linear_backward", torch::wrap_pybind_function_no_gil(gated_linear_backward));
     m.def("gated_input_grad", torch::wrap_pybind_function_no_gil(gated_input_grad));

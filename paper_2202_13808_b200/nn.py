@@ -200,7 +200,7 @@ class DropITGatedLinear(nn.Module):
     products, the gate function f ("silu", "gelu" or "relu") and their product are one kernel.  The two projections are one parameter
     `weight` [2 * hidden, channels] (`bias` [2 * hidden]), the gate's half first.  The gate keeps its own cache, the two projections
     (Sec. 3.5); their gradients with respect to W come from D(x) (Eq. 6), with respect to x from W alone (Eq. 3).  The gradients cannot be
-    differentiated again."""
+    differentiated again, and in training there is no forward-mode derivative (an error says so)."""
 
     def __init__(self, in_features: int, hidden_features: int, bias: bool = True, gate: str = "silu", gamma: float = 0.9,
                  fmt: str = "bitmask", device=None, dtype=None):
@@ -230,17 +230,19 @@ class DropITGatedLinear(nn.Module):
             dt = torch.get_autocast_dtype("cuda")
             x, weight, bias = x.to(dt), weight.to(dt), None if bias is None else bias.to(dt)
         if not (self.training and torch.is_grad_enabled()):
-            if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or (bias is not None and bias.requires_grad)):
-                # gradients outside of training are those of the stock operations (Sec. 3.5: inference is unchanged)
+            native = api._native()
+            if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or (bias is not None and bias.requires_grad)) or \
+                    native.has_tangent(x) or native.has_tangent(weight) or native.has_tangent(bias):
+                # derivatives outside of training are those of the stock operations (Sec. 3.5: inference is unchanged)
                 a, u = F.linear(x, weight, bias).chunk(2, -1)
                 return {"silu": F.silu, "gelu": F.gelu, "relu": F.relu}[self.gate](a) * u
-            return api._native().gated_linear(x, weight, bias, self._gate, False)[0]
+            return native.gated_linear(x, weight, bias, self._gate, False)[0]
         return api._native().gated_layer(x, weight, bias, self.gamma, self._fmt, self._gate)
 
 
 class DropITRotary(nn.Module):
     """Rotary positions with several axes on queries and keys (see api.dropit_rotary and dropit_rotary_plan): (q, k, positions) ->
-    (q', k').  The backward pass is the inverse rotation and keeps the positions only."""
+    (q', k').  The backward pass is the inverse rotation and keeps the positions only; forward-mode derivatives are refused."""
 
     def __init__(self, head_dim: int, sections, theta: float = 10000.0, interleaved: bool = False, shared: bool = False):
         super().__init__()
