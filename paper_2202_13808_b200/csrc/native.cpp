@@ -599,6 +599,7 @@ struct AdamWParams {
     std::vector<Tensor> params;
     std::vector<int64_t> first_block, group;
     std::vector<std::vector<int64_t>> sizes, strides;       // as they were when the moments were laid out
+    std::vector<at::ScalarType> types;
 };
 using AdamWGroupTuple = std::tuple<double, c10::optional<Tensor>, double, double, double, double>;     // lr, lr on the device, decay, betas, eps
 
@@ -621,6 +622,8 @@ void adamw_step(const AdamWParams& all, const std::vector<AdamWGroupTuple>& sett
         const dropit_dtype pt = dtype_code(p, "parameter"), gt = dtype_code(g, "gradient");
         if (p.device() != exp_avg.device()) throw py::value_error("a parameter has moved to another device than its moments");
         if (p.sizes() != all.sizes[i] || p.strides() != all.strides[i]) throw py::value_error("a parameter's shape or strides have changed since its moments were laid out");
+        // bf16 parameters have an fp32 copy, fp32 ones zeros in its place
+        if (master.has_value() && p.scalar_type() != all.types[i]) throw py::value_error("a parameter's type has changed since its copy in fp32 was made");
         if (g.device() != p.device() || g.sizes() != p.sizes()) throw py::value_error("a gradient differs from its parameter in shape or device");
         if (!(p.is_contiguous() && g.is_contiguous()) && g.strides() != p.strides()) {
             Tensor same = at::empty_strided(p.sizes(), p.strides(), g.options());
@@ -682,8 +685,9 @@ PYBIND11_MODULE(_native, m) {
     m.def("rotary", torch::wrap_pybind_function_no_gil(rotary));
     m.def("rotary_layer", torch::wrap_pybind_function_no_gil(rotary_layer));
     py::class_<AdamWParams>(m, "AdamWParams").def(py::init([](std::vector<Tensor> params, std::vector<int64_t> first_block, std::vector<int64_t> group) {
-        AdamWParams all{std::move(params), std::move(first_block), std::move(group), {}, {}};
-        for (const Tensor& p : all.params) all.sizes.push_back(p.sizes().vec()), all.strides.push_back(p.strides().vec());
+        AdamWParams all{std::move(params), std::move(first_block), std::move(group), {}, {}, {}};
+        for (const Tensor& p : all.params)
+            all.sizes.push_back(p.sizes().vec()), all.strides.push_back(p.strides().vec()), all.types.push_back(p.scalar_type());
         return all;
     }));
     m.def("adamw_step", torch::wrap_pybind_function_no_gil(adamw_step));

@@ -20,7 +20,8 @@ class DropITAdamW(torch.optim.Optimizer):
         scale with one fp32 scale per 256 values: exp_avg_scale, exp_avg_root_scale).  Codes are rounded with a dither (a random
         fraction from `seed`, the step, the tensor and the place, so that a run can be repeated): to the nearest code an average that
         moves by a thousandth of itself would not move at all.
-    master: bf16 parameters have an fp32 copy that is stepped in their place (state: master); fp32 ones need none.
+    master: bf16 parameters have an fp32 copy that is stepped in their place (state: master); fp32 ones need none.  The copy is made when the state is
+        laid out: what is written to a parameter later is overwritten from it, and a parameter whose type has changed is refused.
     dither: bf16 parameters are rounded with a dither, which keeps small steps on average without a copy; else to nearest.
     lr may be a CUDA tensor of one fp32 value, which a captured step reads when it replays.  step(grad_factor=t): gradients times t, a CUDA
     tensor of one fp32 value (clipping, unscaling).  Parameters without a gradient stay as they are.  An infinite or NaN gradient
