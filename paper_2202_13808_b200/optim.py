@@ -119,10 +119,11 @@ class DropITAdamW(torch.optim.Optimizer):
                     state[k] = arenas[k][first[i]:first[i] + blocks]
                 else:
                     state[k] = arenas[k][first[i] * BLOCK:first[i] * BLOCK + n].as_strided(p.shape, p.stride())
-            if id(p) in before:
-                for k, v in before[id(p)].items():
-                    state[k].copy_(v)
-            elif "master" in state:
+            held = before.get(id(p), {})
+            for k in state:
+                if k in held:
+                    state[k].copy_(held[k])
+            if "master" in state and "master" not in held:      # new, or fp32 when it was laid out before
                 state["master"].copy_(p)
             self.state[p] = state
         self._arenas, self._steps = arenas, steps

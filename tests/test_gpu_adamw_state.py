@@ -41,3 +41,25 @@ def test_a_copy_in_fp32_belongs_to_the_type_it_was_made_for(cuda_device, bits):
     with pytest.raises(ValueError, match="type"):
         opt.step()
     assert all(torch.equal(p, k) for p, k in zip(model.parameters(), kept))
+
+
+@pytest.mark.parametrize("first, then", [(torch.float32, torch.bfloat16), (torch.bfloat16, torch.float32)])
+def test_a_state_laid_out_again_has_the_copies_of_the_types_there_are(cuda_device, first, then):
+    model = _model(cuda_device, first)
+    opt = dropit.DropITAdamW(model.parameters(), lr=1e-3, weight_decay=0.0, master=True)
+    _fill_grads(model, 1)
+    opt.step()
+    moments = [opt.state[p]["exp_avg"].clone() for p in model.parameters()]
+    model.to(then)
+    opt.add_param_group(dict(params=[torch.nn.Parameter(torch.ones(3, device=cuda_device))]))
+    opt.init_state()
+    for p, m in zip(model.parameters(), moments):
+        assert torch.equal(opt.state[p]["exp_avg"], m) and ("master" in opt.state[p]) == (then == torch.bfloat16)
+        if then == torch.bfloat16:
+            assert torch.equal(opt.state[p]["master"], p.detach().float())
+    kept = [p.detach().clone() for p in model.parameters()]
+    _fill_grads(model, 2)
+    opt.step()
+    # a step is at most lr (1 - b1^t)^-1 sqrt(1 - b2^t) m / sqrt(v) < 5 lr here, and a bf16 value rounds to within 2^-8 of itself
+    for p, k in zip(model.parameters(), kept):
+        assert float((p.detach().float() - k.float()).abs().max()) <= 5e-3 + 2.0 ** -8 * float(k.float().abs().max())
