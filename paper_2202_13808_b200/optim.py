@@ -98,6 +98,8 @@ class DropITAdamW(torch.optim.Optimizer):
         device = params[0].device
         if any(p.device != device for p in params) or device.type != "cuda":
             raise ValueError("all parameters must be on one CUDA device (there is no CPU path)")
+        if torch.cuda.is_current_stream_capturing():        # the zeros and copies below would be part of the graph, and every replay begin anew
+            raise RuntimeError("the state must be laid out before a step is captured: call init_state()")
         spans = sorted((p.data_ptr(), p.data_ptr() + p.numel() * p.element_size()) for p in params if p.numel())
         if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
             raise ValueError("two parameters share memory: one step would take it in turns with itself")
@@ -132,7 +134,7 @@ class DropITAdamW(torch.optim.Optimizer):
         self._plan = api._native().AdamWParams(params, first, group_of)
 
     def init_state(self, p=None):
-        """Allocate the state now (the first step does it otherwise); returns state[p]."""
+        """Lay out the state now; returns state[p].  The first step does it otherwise, and the first one after add_param_group, but not under capture."""
         if self._plan is None:
             self._build()
         return None if p is None else self.state[p]

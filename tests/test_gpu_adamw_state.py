@@ -63,3 +63,28 @@ def test_a_state_laid_out_again_has_the_copies_of_the_types_there_are(cuda_devic
     # a step is at most lr (1 - b1^t)^-1 sqrt(1 - b2^t) m / sqrt(v) < 5 lr here, and a bf16 value rounds to within 2^-8 of itself
     for p, k in zip(model.parameters(), kept):
         assert float((p.detach().float() - k.float()).abs().max()) <= 5e-3 + 2.0 ** -8 * float(k.float().abs().max())
+
+
+@pytest.mark.parametrize("again", [False, True])
+def test_a_state_is_not_laid_out_while_a_step_is_captured(cuda_device, again):
+    """Its zeros would be part of the graph, and every replay would begin anew."""
+    model = _model(cuda_device)
+    opt = dropit.DropITAdamW(model.parameters(), lr=1e-2)
+    _fill_grads(model, 1)
+    late = torch.nn.Parameter(torch.ones(5, device=cuda_device))
+    late.grad = torch.ones_like(late)
+    if again:
+        opt.step()
+        opt.add_param_group(dict(params=[late]))
+    with pytest.raises(RuntimeError, match="init_state"):
+        with torch.cuda.graph(torch.cuda.CUDAGraph()):
+            opt.step()
+    opt.init_state()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        opt.step()
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert int(opt.state[model.weight]["step"]) == 3 + again
+    assert not again or int(opt.state[late]["step"]) == 3
