@@ -2,6 +2,7 @@
 // stream lookup and the autograd nodes (GELU + Linear, gated linear, rotary positions) in C++, on top of the C ABI in include/dropit.h.  A layer call is tens
 // of microseconds of GPU time, less than what marshalling the same calls through ctypes takes on the host.
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDAGraphsC10Utils.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/functions/basic_ops.h>
@@ -603,8 +604,8 @@ struct AdamWParams {
 };
 using AdamWGroupTuple = std::tuple<double, c10::optional<Tensor>, double, double, double, double>;     // lr, lr on the device, decay, betas, eps
 
-// One call of the library for each combination of types and of betas and eps among the parameters that have a gradient.
-void adamw_step(const AdamWParams& all, const std::vector<AdamWGroupTuple>& settings, int64_t state_bits, bool dither, int64_t seed, const Tensor& exp_avg,
+// One call of the library for each combination of types and of betas and eps among the parameters that have a gradient.  True if the step is captured.
+bool adamw_step(const AdamWParams& all, const std::vector<AdamWGroupTuple>& settings, int64_t state_bits, bool dither, int64_t seed, const Tensor& exp_avg,
                 const Tensor& exp_avg_sq, const c10::optional<Tensor>& exp_avg_scale, const c10::optional<Tensor>& exp_avg_sq_scale,
                 const c10::optional<Tensor>& master, const Tensor& steps, const Tensor& ticket, const c10::optional<Tensor>& grad_factor) {
     struct Call {
@@ -655,6 +656,7 @@ void adamw_step(const AdamWParams& all, const std::vector<AdamWGroupTuple>& sett
     }
     for (size_t i = 0; i < all.params.size(); ++i)
         if (all.params[i].grad().defined()) all.params[i].unsafeGetTensorImpl()->bump_version();
+    return !calls.empty() && c10::cuda::currentStreamCaptureStatusMayInitCtx() != c10::cuda::CaptureStatus::None;
 }
 
 }  // namespace

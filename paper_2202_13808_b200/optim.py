@@ -27,17 +27,20 @@ class DropITAdamW(torch.optim.Optimizer):
     tensor of one fp32 value (clipping, unscaling).  Parameters without a gradient stay as they are.  An infinite or NaN gradient
     spoils its own value, and in 8 bits the moments of its block of 256.
 
-    The state lies in arenas, one per kind, in the order of the parameters, blocks of 256 values; state[p] holds views of them."""
+    The state lies in arenas, one per kind, in the order of the parameters, blocks of 256 values; state[p] holds views of them.  A group that is
+    added later moves them, which a captured step forbids."""
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 1e-2, state_bits: int = 32,
                  master: bool = False, dither: bool = False, seed: int = 0):
         if state_bits not in (8, 32):
             raise ValueError("state_bits must be 8 or 32, got %r" % (state_bits,))
         self.state_bits, self.master, self.dither, self.seed = int(state_bits), bool(master), bool(dither), int(seed) & 0xFFFFFFFF
-        self._plan, self._arenas = None, {}
+        self._plan, self._arenas, self._captured = None, {}, False
         super().__init__(params, dict(lr=lr, betas=betas, eps=eps, weight_decay=weight_decay))
 
     def add_param_group(self, param_group):
+        if self._captured:
+            raise RuntimeError("a captured step holds the places of the state, which another group would move: add groups, then capture")
         super().add_param_group(param_group)
         try:
             self._check_group(self.param_groups[-1])
@@ -72,6 +75,7 @@ class DropITAdamW(torch.optim.Optimizer):
     def __setstate__(self, state):
         super().__setstate__(state)
         self._plan, self._arenas = None, {}      # laid out anew, from the state, when they are next needed
+        self.__dict__.setdefault("_captured", False)
 
     # ---- state ----
 
@@ -189,10 +193,11 @@ class DropITAdamW(torch.optim.Optimizer):
                 lr, device_lr = 0.0, self._scalar(lr, "lr")
             settings.append((lr, device_lr, g["weight_decay"], *g["betas"], g["eps"]))
         a = self._arenas
-        api._native().adamw_step(self._plan, settings, self.state_bits, self.dither, self.seed, a["exp_avg"],
-                                 a["exp_avg_root" if self.state_bits == 8 else "exp_avg_sq"], a.get("exp_avg_scale"),
-                                 a.get("exp_avg_root_scale"), a.get("master"), self._steps, self._ticket,
-                                 None if grad_factor is None else self._scalar(grad_factor, "grad_factor"))
+        captured = api._native().adamw_step(
+            self._plan, settings, self.state_bits, self.dither, self.seed, a["exp_avg"], a["exp_avg_root" if self.state_bits == 8 else "exp_avg_sq"],
+            a.get("exp_avg_scale"), a.get("exp_avg_root_scale"), a.get("master"), self._steps, self._ticket,
+            None if grad_factor is None else self._scalar(grad_factor, "grad_factor"))
+        self._captured |= captured
         return loss
 
     def _scalar(self, t, name):

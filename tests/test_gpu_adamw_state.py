@@ -88,3 +88,23 @@ def test_a_state_is_not_laid_out_while_a_step_is_captured(cuda_device, again):
     torch.cuda.synchronize()
     assert int(opt.state[model.weight]["step"]) == 3 + again
     assert not again or int(opt.state[late]["step"]) == 3
+
+
+def test_a_group_that_comes_after_a_capture_is_refused(cuda_device):
+    """The state would move from under the captured step, whose replays would go on in memory that is somebody else's."""
+    model = _model(cuda_device)
+    opt = dropit.DropITAdamW(model.parameters(), lr=1e-2)
+    _fill_grads(model, 1)
+    opt.step()
+    opt.add_param_group(dict(params=[torch.nn.Parameter(torch.ones(3, device=cuda_device))]))        # nothing is captured yet
+    opt.step()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        opt.step()
+    with pytest.raises(RuntimeError, match="captured"):
+        opt.add_param_group(dict(params=[torch.nn.Parameter(torch.ones(5, device=cuda_device))]))
+    assert len(opt.param_groups) == 2
+    graph.replay()
+    opt.step()
+    torch.cuda.synchronize()
+    assert int(opt.state[model.weight]["step"]) == 4
