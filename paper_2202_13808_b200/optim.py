@@ -149,25 +149,37 @@ class DropITAdamW(torch.optim.Optimizer):
         self.init_state()
         return self._arenas.get(kind)
 
+    @torch.no_grad()
     def load_state_dict(self, state_dict):
-        """Takes the hyperparameters and copies the state into this optimizer's arenas, type for type."""
-        saved = dict(state_dict)
-        values = saved["state"]
-        super().load_state_dict({**saved, "state": {}})
-        self.state.clear()
-        self._plan = None
-        self._build()
-        for i, p in enumerate(self._all_params()):
-            given = values.get(i)
-            if not given:
-                continue
-            if set(given) != set(self.state[p]):
-                raise ValueError("the state has %s, this optimizer %s" % (sorted(given), sorted(self.state[p])))
-            for k, v in given.items():
-                mine = self.state[p][k]
-                if v.shape != mine.shape or v.dtype != mine.dtype:
-                    raise ValueError("%s of parameter %d is %s %s, expected %s %s" % (k, i, v.dtype, tuple(v.shape), mine.dtype, tuple(mine.shape)))
-                mine.copy_(v)
+        """Takes the hyperparameters and copies the state into this optimizer's arenas, type for type.  State and learning rates that are tensors
+        keep their places, so that a captured step goes on from what is loaded.  Parameters that the checkpoint has no state for begin anew."""
+        self.init_state()
+        values, params = state_dict["state"], self._all_params()
+        laid_out = self.state, self._plan, self._arenas
+        lrs = [g["lr"] for g in self.param_groups]
+        super().load_state_dict({**state_dict, "state": {}})
+        self.state, self._plan, self._arenas = laid_out
+        self._keep_lr_tensors(lrs)
+        ids = [i for g in state_dict["param_groups"] for i in g["params"]]
+        for i, p in enumerate(params):
+            mine, given = self.state[p], values.get(ids[i])
+            if given and set(given) != set(mine):
+                raise ValueError("the state has %s, this optimizer %s" % (sorted(given), sorted(mine)))
+            for k, v in mine.items():
+                if not given:
+                    v.copy_(p) if k == "master" else v.zero_()
+                elif given[k].shape != v.shape or given[k].dtype != v.dtype:
+                    raise ValueError("%s of parameter %d is %s %s, expected %s %s" % (k, i, given[k].dtype, tuple(given[k].shape), v.dtype, tuple(v.shape)))
+                else:
+                    v.copy_(given[k])
+
+    def _keep_lr_tensors(self, before):
+        """Learning rates that were tensors take the loaded values; groups that shared one and no longer agree get tensors of their own."""
+        loaded = [float(g["lr"]) for g in self.param_groups]
+        for g, lr, value in zip(self.param_groups, before, loaded):
+            if isinstance(lr, torch.Tensor):
+                agree = all(v == value for v, other in zip(loaded, before) if other is lr)
+                g["lr"] = lr.fill_(value) if agree else torch.full_like(lr, value)
 
     # ---- the step ----
 

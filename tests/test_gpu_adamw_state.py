@@ -108,3 +108,83 @@ def test_a_group_that_comes_after_a_capture_is_refused(cuda_device):
     opt.step()
     torch.cuda.synchronize()
     assert int(opt.state[model.weight]["step"]) == 4
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_a_checkpoint_is_copied_into_the_state_there_is(cuda_device, bits, dtype):
+    model = _model(cuda_device, dtype)
+    opt = dropit.DropITAdamW(model.parameters(), lr=1e-2, state_bits=bits, master=True, seed=1)
+    _fill_grads(model, 1)
+    opt.step()
+    saved, params = copy.deepcopy(opt.state_dict()), [p.detach().clone() for p in model.parameters()]
+    places = [[v.data_ptr() for v in opt.state[p].values()] for p in model.parameters()]
+    arena = opt.whole_state("exp_avg").data_ptr()
+    opt.step()
+    want = [p.detach().clone() for p in model.parameters()], _values(opt, model.parameters())
+    opt.step()
+    opt.load_state_dict(saved)
+    assert [[v.data_ptr() for v in opt.state[p].values()] for p in model.parameters()] == places
+    assert opt.whole_state("exp_avg").data_ptr() == arena
+    with torch.no_grad():
+        for p, k in zip(model.parameters(), params):
+            p.copy_(k)
+    opt.step()
+    assert all(torch.equal(p, w) for p, w in zip(model.parameters(), want[0])) and _equal(_values(opt, model.parameters()), want[1])
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_a_captured_step_goes_on_from_a_checkpoint(cuda_device, bits):
+    model = _model(cuda_device)
+    lr = torch.tensor(1e-2, device=cuda_device)
+    opt = dropit.DropITAdamW(model.parameters(), lr=lr, state_bits=bits)
+    _fill_grads(model, 1)
+    opt.step()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        opt.step()
+    saved, params = copy.deepcopy(opt.state_dict()), [p.detach().clone() for p in model.parameters()]
+    for _ in range(2):
+        graph.replay()
+    want = [p.detach().clone() for p in model.parameters()], _values(opt, model.parameters())
+    lr.fill_(0.5)
+    opt.load_state_dict(saved)
+    assert opt.param_groups[0]["lr"] is lr and float(lr) == float(torch.tensor(1e-2))       # what the graph reads
+    with torch.no_grad():
+        for p, k in zip(model.parameters(), params):
+            p.copy_(k)
+    for _ in range(2):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert int(opt.state[model.weight]["step"]) == 3
+    assert all(torch.equal(p, w) for p, w in zip(model.parameters(), want[0])) and _equal(_values(opt, model.parameters()), want[1])
+
+
+def test_a_checkpoint_without_a_state_begins_anew(cuda_device):
+    model = _model(cuda_device, torch.bfloat16)
+    fresh = dropit.DropITAdamW(model.parameters(), lr=3e-2, master=True).state_dict()
+    assert not fresh["state"]
+    opt = dropit.DropITAdamW(model.parameters(), lr=1e-2, master=True)
+    _fill_grads(model, 1)
+    opt.step()
+    opt.load_state_dict(fresh)
+    assert opt.param_groups[0]["lr"] == 3e-2
+    for p in model.parameters():
+        s = opt.state[p]
+        assert int(s["step"]) == 0 and not bool(s["exp_avg"].any()) and not bool(s["exp_avg_sq"].any())
+        assert torch.equal(s["master"], p.detach().float())
+
+
+def test_learning_rates_that_are_tensors_keep_their_places(cuda_device):
+    a, b, c = (torch.nn.Parameter(torch.ones(n, device=cuda_device)) for n in (3, 4, 5))
+    shared, own = torch.tensor(1e-2, device=cuda_device), torch.tensor([1e-3], device=cuda_device)
+    opt = dropit.DropITAdamW([dict(params=[a], lr=shared), dict(params=[b], lr=shared), dict(params=[c], lr=own)])
+    saved = opt.state_dict()
+    for lr, other, third in ((0.3, 0.3, torch.tensor(0.7)), (0.1, 0.2, 0.9)):
+        for g, v in zip(saved["param_groups"], (lr, other, third)):
+            g["lr"] = v
+        opt.load_state_dict(saved)
+        got = [g["lr"] for g in opt.param_groups]
+        assert [float(v) for v in got] == [float(torch.tensor(float(v))) for v in (lr, other, third)]
+        assert got[2] is own and (got[0] is shared) == (got[1] is shared) == (lr == other)
+        assert all(v.device == a.device for v in got)
