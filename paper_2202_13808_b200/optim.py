@@ -152,26 +152,36 @@ class DropITAdamW(torch.optim.Optimizer):
     @torch.no_grad()
     def load_state_dict(self, state_dict):
         """Takes the hyperparameters and copies the state into this optimizer's arenas, type for type.  State and learning rates that are tensors
-        keep their places, so that a captured step goes on from what is loaded.  Parameters that the checkpoint has no state for begin anew."""
+        keep their places, so that a captured step goes on from what is loaded.  Parameters that the checkpoint has no state for begin anew; a checkpoint
+        that does not fit is refused before anything changes."""
         self.init_state()
-        values, params = state_dict["state"], self._all_params()
+        params, groups, lrs = self._all_params(), state_dict["param_groups"], [g["lr"] for g in self.param_groups]
+        if [len(g["params"]) for g in groups] != [len(g["params"]) for g in self.param_groups]:
+            raise ValueError("the checkpoint has other groups of parameters")
+        given = [state_dict["state"].get(i) for g in groups for i in g["params"]]
+        for i, (p, held) in enumerate(zip(params, given)):
+            mine = self.state[p]
+            if held and set(held) != set(mine):
+                raise ValueError("the state has %s, this optimizer %s" % (sorted(held), sorted(mine)))
+            for k, v in (held or {}).items():
+                if v.shape != mine[k].shape or v.dtype != mine[k].dtype:
+                    raise ValueError("%s of parameter %d is %s %s, expected %s %s" % (k, i, v.dtype, tuple(v.shape), mine[k].dtype, tuple(mine[k].shape)))
+        if self._captured and any(lr is other and float(g["lr"]) != float(h["lr"]) for g, lr in zip(groups, lrs) for h, other in zip(groups, lrs)
+                                  if isinstance(lr, torch.Tensor)):
+            raise ValueError("groups whose learning rate a captured step reads from one tensor are to have different ones")
+        # nothing has changed up to here
         laid_out = self.state, self._plan, self._arenas
-        lrs = [g["lr"] for g in self.param_groups]
         super().load_state_dict({**state_dict, "state": {}})
         self.state, self._plan, self._arenas = laid_out
         self._keep_lr_tensors(lrs)
-        ids = [i for g in state_dict["param_groups"] for i in g["params"]]
-        for i, p in enumerate(params):
-            mine, given = self.state[p], values.get(ids[i])
-            if given and set(given) != set(mine):
-                raise ValueError("the state has %s, this optimizer %s" % (sorted(given), sorted(mine)))
-            for k, v in mine.items():
-                if not given:
-                    v.copy_(p) if k == "master" else v.zero_()
-                elif given[k].shape != v.shape or given[k].dtype != v.dtype:
-                    raise ValueError("%s of parameter %d is %s %s, expected %s %s" % (k, i, given[k].dtype, tuple(given[k].shape), v.dtype, tuple(v.shape)))
+        for p, held in zip(params, given):
+            for k, v in self.state[p].items():
+                if held:
+                    v.copy_(held[k])
+                elif k == "master":
+                    v.copy_(p)
                 else:
-                    v.copy_(given[k])
+                    v.zero_()
 
     def _keep_lr_tensors(self, before):
         """Learning rates that were tensors take the loaded values; groups that shared one and no longer agree get tensors of their own."""

@@ -188,3 +188,44 @@ def test_learning_rates_that_are_tensors_keep_their_places(cuda_device):
         assert [float(v) for v in got] == [float(torch.tensor(float(v))) for v in (lr, other, third)]
         assert got[2] is own and (got[0] is shared) == (got[1] is shared) == (lr == other)
         assert all(v.device == a.device for v in got)
+
+
+def test_a_learning_rate_that_a_captured_step_reads_is_not_torn_in_two(cuda_device):
+    params = [torch.nn.Parameter(torch.ones(n, device=cuda_device)) for n in (3, 4)]
+    lr = torch.tensor(1e-2, device=cuda_device)
+    opt = dropit.DropITAdamW([dict(params=[p], lr=lr) for p in params])
+    for p in params:
+        p.grad = torch.ones_like(p)
+    opt.step()
+    with torch.cuda.graph(torch.cuda.CUDAGraph()):
+        opt.step()
+    saved = opt.state_dict()
+    saved["param_groups"][0]["lr"] = 0.5
+    with pytest.raises(ValueError, match="captured"):
+        opt.load_state_dict(saved)
+    assert all(g["lr"] is lr for g in opt.param_groups) and float(lr) == float(torch.tensor(1e-2))
+
+
+@pytest.mark.parametrize("how", ["shape", "type", "name", "count"])
+def test_a_checkpoint_that_is_refused_changes_nothing(cuda_device, how):
+    model = _model(cuda_device)
+    opt = dropit.DropITAdamW(model.parameters(), lr=1e-2)
+    _fill_grads(model, 1)
+    opt.step()
+    saved = copy.deepcopy(opt.state_dict())
+    saved["param_groups"][0]["lr"] = 7.0
+    last = saved["state"][1]
+    if how == "shape":
+        last["exp_avg_sq"] = last["exp_avg_sq"][:-1]
+    elif how == "type":
+        last["exp_avg_sq"] = last["exp_avg_sq"].double()
+    elif how == "name":
+        last["other"] = last.pop("exp_avg_sq")
+    else:
+        saved["param_groups"][0]["params"] = [0]
+    before = _values(opt, model.parameters())
+    with pytest.raises(ValueError):
+        opt.load_state_dict(saved)
+    assert opt.param_groups[0]["lr"] == 1e-2 and _equal(_values(opt, model.parameters()), before)
+    opt.step()
+    assert int(opt.state[model.weight]["step"]) == 2
