@@ -154,6 +154,10 @@ class DropITAdamW(torch.optim.Optimizer):
         """Takes the hyperparameters and copies the state into this optimizer's arenas, type for type.  State and learning rates that are tensors
         keep their places, so that a captured step goes on from what is loaded.  Parameters that the checkpoint has no state for begin anew; a checkpoint
         that does not fit is refused before anything changes."""
+        state_dict, hooks = dict(state_dict), (self._optimizer_load_state_dict_pre_hooks, self._optimizer_load_state_dict_post_hooks)
+        for hook in hooks[0].values():
+            changed = hook(self, state_dict)
+            state_dict = state_dict if changed is None else changed
         self.init_state()
         params, groups, lrs = self._all_params(), state_dict["param_groups"], [g["lr"] for g in self.param_groups]
         if [len(g["params"]) for g in groups] != [len(g["params"]) for g in self.param_groups]:
@@ -171,8 +175,13 @@ class DropITAdamW(torch.optim.Optimizer):
             raise ValueError("groups whose learning rate a captured step reads from one tensor are to have different ones")
         # nothing has changed up to here
         laid_out = self.state, self._plan, self._arenas
-        super().load_state_dict({**state_dict, "state": {}})
-        self.state, self._plan, self._arenas = laid_out
+        empty = type(hooks[0])()
+        try:            # the base class takes the groups; its hooks see the whole of it, from here
+            self._optimizer_load_state_dict_pre_hooks = self._optimizer_load_state_dict_post_hooks = empty
+            super().load_state_dict({**state_dict, "state": {}})
+        finally:
+            self._optimizer_load_state_dict_pre_hooks, self._optimizer_load_state_dict_post_hooks = hooks
+            self.state, self._plan, self._arenas = laid_out
         self._keep_lr_tensors(lrs)
         for p, held in zip(params, given):
             for k, v in self.state[p].items():
@@ -182,6 +191,8 @@ class DropITAdamW(torch.optim.Optimizer):
                     v.copy_(p)
                 else:
                     v.zero_()
+        for hook in hooks[1].values():
+            hook(self)
 
     def _keep_lr_tensors(self, before):
         """Learning rates that were tensors take the loaded values; groups that shared one and no longer agree get tensors of their own."""

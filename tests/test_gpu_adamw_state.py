@@ -229,3 +229,22 @@ def test_a_checkpoint_that_is_refused_changes_nothing(cuda_device, how):
     assert opt.param_groups[0]["lr"] == 1e-2 and _equal(_values(opt, model.parameters()), before)
     opt.step()
     assert int(opt.state[model.weight]["step"]) == 2
+
+
+def test_hooks_around_a_checkpoint_see_its_state(cuda_device):
+    model = _model(cuda_device)
+    opt = dropit.DropITAdamW(model.parameters(), lr=1e-2)
+    _fill_grads(model, 1)
+    opt.step()
+    saved = copy.deepcopy(opt.state_dict())
+    opt.step()
+    seen = []
+
+    def before(o, state_dict):
+        seen.append(sorted(state_dict["state"]))
+        state_dict["state"][0]["step"] = state_dict["state"][0]["step"] + 4
+        return state_dict
+    opt.register_load_state_dict_pre_hook(before)
+    opt.register_load_state_dict_post_hook(lambda o: seen.append(int(o.state[model.weight]["step"])))
+    opt.load_state_dict(saved)
+    assert seen == [[0, 1], 5]
