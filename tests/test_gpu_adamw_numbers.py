@@ -1,0 +1,113 @@
+"""AdamW at the ends of fp32's range, and the forms of the step one by one: 8-bit moments against the same operations in fp32, bit by bit."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2202_13808_b200 as dropit
+from test_gpu_adamw import BLOCK, _code_values, _step64, _words
+
+pytestmark = pytest.mark.gpu
+
+f32 = np.float32
+
+
+def _codes(values, scale, amax, words16, keep_above_zero):
+    """Codes of a block's values as include/dropit.h states them, every operation rounded to fp32: a product with the scale's reciprocal, and the
+    place between two codes plus the random fraction."""
+    with np.errstate(divide="ignore", over="ignore", invalid="ignore"):
+        y = (np.abs(values) * np.where(scale > 0, f32(1) / scale, f32(0)).astype(f32)).astype(f32)
+    table = _code_values().astype(np.float64)
+    y = y.astype(np.float64)
+    low = np.clip(np.searchsorted(table, y, side="right") - 1, 0, len(table) - 1)
+    high = np.minimum(low + 1, len(table) - 1)
+    gap = np.where(high > low, table[high] - table[low], 1.0)
+    # the place is held in 20 bits of the normal codes, and rounded to them below
+    place = np.clip((y - table[low]) / gap, 0, 1)
+    held = np.rint(place * 2 ** 20) / 2 ** 20
+    code = table[np.where(held + words16.astype(np.float64) / 65536 >= 1, high, low)]
+    if keep_above_zero:
+        code = np.where((values > 0) & (code == 0), table[1], code)
+    sure = (held == place) | (np.abs(held + words16 / 65536.0 - 1) > 2.0 ** -19)
+    return code * np.sign(np.where(values == 0, 0, values)), sure
+
+
+def _emulate(g, m0, r0, b1, b2, factor):
+    """m and the root in fp32, each operation rounded by itself."""
+    with np.errstate(over="ignore", under="ignore"):
+        one1, one2 = f32(1.0 - b1), f32(1.0 - b2)
+        if factor is not None:
+            g = (g * f32(factor)).astype(f32)
+        m = ((f32(b1) * m0).astype(f32) + (one1 * g).astype(f32)).astype(f32)
+        v = ((f32(b2) * (r0 * r0).astype(f32)).astype(f32) + ((one2 * g).astype(f32) * g).astype(f32)).astype(f32)
+        return m, np.sqrt(v)
+
+
+@pytest.mark.parametrize("span", [(-3, 3), (-62, -30), (-75, -60), (0, 60)])
+@pytest.mark.parametrize("factor", [None])
+def test_8_bit_moments_are_those_of_fp32_operations(cuda_device, span, factor):
+    """Scales bit by bit and codes wherever the 20 bits of a place decide, for gradients of 2^-75 to 2^60: every block has a size of its own.  Roots are
+    exact roots of fp32 rounded once, of v below 2^-126 too."""
+    blocks, b1, b2 = 4000, 0.9, 0.99
+    n = blocks * BLOCK
+    rng = np.random.RandomState(span[0] + 100)
+    p = torch.nn.Parameter(torch.zeros(n, device=cuda_device))
+    opt = dropit.DropITAdamW([p], lr=0.0, betas=(b1, b2), weight_decay=0.0, state_bits=8, seed=11)
+    s = opt.init_state(p)
+    scale_by = None if factor is None else torch.tensor(factor, device=cuda_device)
+    for t in range(1, 4):
+        size = np.exp2(rng.uniform(span[0], span[1], (blocks, 1)))
+        g = (rng.randn(blocks, BLOCK) * size).astype(f32)
+        block = lambda k, scale: (s[k].float().cpu().numpy().reshape(blocks, BLOCK) * s[scale].cpu().numpy()[:, None]).astype(f32)
+        m, r = _emulate(g, block("exp_avg", "exp_avg_scale"), block("exp_avg_root", "exp_avg_root_scale"), b1, b2, factor)
+        p.grad = torch.from_numpy(g.reshape(-1)).to(cuda_device)
+        opt.step(grad_factor=scale_by)
+        words, _ = _words(11, t, 0, n)
+        for x, k, bits in ((m, "exp_avg", words >> 16), (r, "exp_avg_root", words & 0xFFFF)):
+            top = np.abs(x).max(1)
+            want = np.where(top < 1e-30, f32(0), (top * f32(1 / 448)).astype(f32))
+            got = s[k + "_scale"].cpu().numpy()
+            assert (got == want).all(), (k, int((got != want).sum()))
+            code, sure = _codes(x, want[:, None], top[:, None], bits.reshape(blocks, BLOCK), k != "exp_avg")
+            held = s[k].double().cpu().numpy().reshape(blocks, BLOCK)
+            assert (held == code)[sure & (want[:, None] > 0)].all()
+            assert sure.mean() > 0.99
+            assert not held[want == 0].any()
+
+
+@pytest.mark.parametrize("low, high", [(-126, -90), (-102, 0), (-2, 2), (0, 127)])
+def test_roots_and_reciprocals_over_their_range(cuda_device, low, high):
+    """One value in each of half a million blocks, b1 = b2 = 0: the scales are the values' and their roots' of fp32, and the value's own code is 448.  Roots of squares'
+    neighbours, where a second moment is nearest to one whose root lies between two floats, among them."""
+    n = 1 << 19
+    rng = np.random.RandomState(high + 200)
+    g = np.exp2(rng.uniform(low / 2, min(high / 2, 63.4), n)).astype(f32) * rng.choice([-1, 1], n).astype(f32)
+    g[::4] = (np.round(np.exp2(rng.uniform(11, 12, n // 4))) * np.exp2(np.floor(np.log2(np.abs(g[::4]))) - 11)).astype(f32)
+    p = torch.nn.Parameter(torch.zeros(n * BLOCK, device=cuda_device))
+    opt = dropit.DropITAdamW([p], lr=0.0, betas=(0.0, 0.0), weight_decay=0.0, state_bits=8, seed=1)
+    p.grad = torch.zeros_like(p)
+    p.grad.view(n, BLOCK)[:, 7] = torch.from_numpy(g).to(cuda_device)
+    opt.step()
+    s = opt.state[p]
+    with np.errstate(under="ignore"):
+        root = np.sqrt((g * g).astype(f32))
+        want = [(x * f32(1 / 448)).astype(f32) for x in (np.abs(g), root)]
+    for k, w in zip(("exp_avg", "exp_avg_root"), want):
+        assert (s[k + "_scale"].cpu().numpy() == w).all()
+        # value times reciprocal is 448 but for three halves of a unit; the code below takes a fraction of 2^-16 and less
+        codes = s[k].view(n, BLOCK)[:, 7].float().abs().cpu().numpy()
+        assert ((codes == 448) | (codes == 416)).all() and (codes == 448).mean() > 0.999
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("size", [1e-17, 3e-19, 1e-20, 1e-21])
+def test_gradients_whose_squares_are_tiny(cuda_device, bits, size):
+    """v falls below 2^-126, where fp32 has fewer digits but still a root.  eps = 0: the first step moves every value by lr, whatever the gradients' size."""
+    p = torch.nn.Parameter(torch.zeros(2 * BLOCK, device=cuda_device))
+    opt = dropit.DropITAdamW([p], lr=1.0, betas=(0.9, 0.99), eps=0.0, weight_decay=0.0, state_bits=bits)
+    p.grad = torch.full_like(p, size)
+    opt.step()
+    # v = 0.01 size^2 is off by half of 2^-149, 7.0e-46: for 1e-21 (1e-44) a part in 14, half of that for the root
+    assert bool(((p.detach() + 1).abs() <= 1e-5 + 0.6 * 7.1e-46 / (0.01 * size * size) + 7.1e-46 / (size * size) * (bits == 32)).all())
+    s = opt.state[p]
+    root = s["exp_avg_root"].double() * s["exp_avg_root_scale"].double()[0] if bits == 8 else s["exp_avg_sq"].double().sqrt()
+    assert bool((root / (0.1 * size) - 1).abs().max() <= 0.12)          # half of 7 % of v, and the next code below the largest
