@@ -183,7 +183,7 @@ __device__ __forceinline__ float approx_sqrt(float x) {
 // The root to the nearest fp32 for x of 2^-102 and more: x times its approximate reciprocal root, and a Newton step whose residue is exact (P. Markstein,
 // "Computation of elementary functions on the IBM RISC System/6000 processor", 1990): compared with __fsqrt_rn for all of them.  Smaller ones, whose residue
 // has digits under 2^-149, take 2^64 first where ANY; so do zero, infinity and NaN, which are their own roots and come out as NaN without it.
-// 86.6 M values: 215 us; with __fsqrt_rn 220, with __frcp_rn too 224.
+// 86.6 M values: 217 us; with __fsqrt_rn 5 more, with __frcp_rn too 9.
 constexpr float kSmallestFast = 0x1p-102f;
 template <bool ANY>
 __device__ __forceinline__ float rounded_sqrt(float x) {
@@ -227,7 +227,8 @@ __device__ __forceinline__ float block_scale(float top, float (&values)[8], floa
 
 // What holds for a tensor.
 struct Step {
-    float beta1, beta2, gain1, gain2;       // gain: (1 - beta) times the gradients' factor, squared for the second moment
+    float beta1, beta2, gain1, gain2;       // gain: 1 - beta
+    float factor;                           // of the gradients
     float eps, decay, rate, root_correction;
     uint32_t key;
     void* p;
@@ -287,7 +288,7 @@ __device__ __forceinline__ void compute_as(const Step& k, const Raw<P, G, BITS8,
         }
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            const float g = value_of(raw.g, i + e);
+            const float g = mul(value_of(raw.g, i + e), k.factor);      // before it is squared: what the factor brings back into fp32's range may have no square there
             float m, v, root;
             if constexpr (BITS8) {
                 // every product, sum and root is rounded by itself: a code turns on the last bit, and one of a block's largest value changes all
@@ -407,11 +408,11 @@ __global__ void __launch_bounds__(kThreads, BITS8 ? kResident8 : kResident32)
 adamw_kernel(const __grid_constant__ Args a) {
     const int lane = threadIdx.x & 31;
     Step k;
-    const float grad_factor = a.grad_factor ? *a.grad_factor : 1.f;
+    k.factor = a.grad_factor ? *a.grad_factor : 1.f;
     k.beta1 = a.beta1;
     k.beta2 = a.beta2;
-    k.gain1 = a.one_minus_beta1 * grad_factor;
-    k.gain2 = a.one_minus_beta2 * grad_factor * grad_factor;
+    k.gain1 = a.one_minus_beta1;
+    k.gain2 = a.one_minus_beta2;
     k.eps = a.eps;
     uint32_t entry = 0, entry_end = 0;
     Raw<P, G, BITS8, FORM> raw;

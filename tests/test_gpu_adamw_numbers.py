@@ -43,7 +43,7 @@ def _emulate(g, m0, r0, b1, b2, factor):
 
 
 @pytest.mark.parametrize("span", [(-3, 3), (-62, -30), (-75, -60), (0, 60)])
-@pytest.mark.parametrize("factor", [None])
+@pytest.mark.parametrize("factor", [None, 0.37])
 def test_8_bit_moments_are_those_of_fp32_operations(cuda_device, span, factor):
     """Scales bit by bit and codes wherever the 20 bits of a place decide, for gradients of 2^-75 to 2^60: every block has a size of its own.  Roots are
     exact roots of fp32 rounded once, of v below 2^-126 too."""
@@ -111,3 +111,20 @@ def test_gradients_whose_squares_are_tiny(cuda_device, bits, size):
     s = opt.state[p]
     root = s["exp_avg_root"].double() * s["exp_avg_root_scale"].double()[0] if bits == 8 else s["exp_avg_sq"].double().sqrt()
     assert bool((root / (0.1 * size) - 1).abs().max() <= 0.12)          # half of 7 % of v, and the next code below the largest
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("size, factor", [(1e20, 1e-20), (1e-3, 1e3), (3e30, 1e-31), (1e-18, 1e18)])
+def test_a_factor_holds_for_the_gradients_and_not_for_their_squares(cuda_device, bits, size, factor):
+    """Gradients of a loss that is scaled or far off: their squares leave fp32's range, what they are after the factor does not."""
+    g = torch.randn(3 * BLOCK, generator=torch.Generator(device=cuda_device).manual_seed(1), device=cuda_device)
+    p, q = (torch.nn.Parameter(torch.zeros(3 * BLOCK, device=cuda_device)) for _ in range(2))
+    make = lambda t: dropit.DropITAdamW([t], lr=1e-2, weight_decay=0.0, state_bits=bits, seed=3)
+    a, b = make(p), make(q)
+    p.grad = g * size
+    factor = torch.tensor(factor, device=cuda_device)
+    q.grad = p.grad * factor
+    a.step(grad_factor=factor)
+    b.step()
+    assert torch.equal(p, q)
+    assert all(torch.equal(x.float(), y.float()) for x, y in zip(a.state[p].values(), b.state[q].values()))
