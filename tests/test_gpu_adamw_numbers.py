@@ -128,3 +128,84 @@ def test_a_factor_holds_for_the_gradients_and_not_for_their_squares(cuda_device,
     b.step()
     assert torch.equal(p, q)
     assert all(torch.equal(x.float(), y.float()) for x, y in zip(a.state[p].values(), b.state[q].values()))
+
+
+FORMS = [(bits, master, dither) for bits in (8, 32) for master in (False, True) for dither in (False, True)]
+
+
+@pytest.mark.parametrize("bits, master, dither", FORMS)
+@pytest.mark.parametrize("g_type", [torch.float32, torch.bfloat16])
+def test_every_form_of_a_bf16_step(cuda_device, bits, master, dither, g_type):
+    """Parameters rounded to nearest or with a dither, stepped as they are or in an fp32 copy; from held moments, against 64 bits."""
+    shapes = [(5,), (300,), (64, 33), (2, 3, 5, 7)]
+    gen = torch.Generator(device=cuda_device).manual_seed(2)
+    draw = lambda s: torch.randn(s, generator=gen, device=cuda_device)
+    params = [torch.nn.Parameter((draw(s) * 0.1).bfloat16()) for s in shapes]
+    opt = dropit.DropITAdamW(params, lr=3e-3, betas=(0.9, 0.99), weight_decay=0.1, state_bits=bits, master=master, dither=dither, seed=21)
+    opt.init_state()
+    factor = torch.tensor(0.7, device=cuda_device)
+    for t in range(1, 4):
+        held = []
+        for p in params:
+            p.grad_dtype = None
+            p.grad = (draw(p.shape) * 0.02).to(g_type)
+            s = opt.state[p]
+            block = torch.arange(p.numel(), device=cuda_device) // BLOCK
+            if bits == 8:
+                m0 = s["exp_avg"].double().reshape(-1) * s["exp_avg_scale"].double()[block]
+                v0 = (s["exp_avg_root"].double().reshape(-1) * s["exp_avg_root_scale"].double()[block]) ** 2
+            else:
+                m0, v0 = s["exp_avg"].double().reshape(-1), s["exp_avg_sq"].double().reshape(-1)
+            held.append(((s["master"] if master else p.detach()).double().reshape(-1).clone(), m0.clone(), v0.clone()))
+        opt.step(grad_factor=factor)
+        for ordinal, (p, (p0, m0, v0)) in enumerate(zip(params, held)):
+            g = (p.grad.float() * factor).double().reshape(-1)
+            want, m, v, bound = _step64(p0, g, m0, v0, t, 3e-3, 0.1, 0.9, 0.99, 1e-8)
+            s, n = opt.state[p], p.numel()
+            _, other = _words(21, t, ordinal, n)
+            fraction = (other >> np.uint32(16)).astype(np.uint32)
+            now = p.detach().reshape(-1)
+            if master:
+                copy = s["master"].reshape(-1)
+                assert bool(((copy.double() - want).abs() <= bound).all())
+                if dither:              # the copy's pattern plus the fraction, cut to its high half
+                    sums = copy.cpu().numpy().view(np.uint32) + fraction
+                    assert (now.view(torch.int16).cpu().numpy().view(np.uint16) == (sums >> np.uint32(16)).astype(np.uint16)).all()
+                else:
+                    assert torch.equal(now, copy.bfloat16())
+            elif dither:
+                w = want.cpu().numpy()
+                unit = np.exp2(np.floor(np.log2(np.maximum(np.abs(w), 1e-38))) - 7)
+                total = np.abs(w) / unit + fraction / 65536.0
+                # the fp32 value is off by `bound`, and its last 2^-16 of a unit count
+                sure = np.abs(total - np.round(total)) > bound.cpu().numpy() / unit + 2.0 ** -15
+                assert sure.mean() > 0.9 or n < 100
+                assert (now.double().abs().cpu().numpy() == np.floor(total) * unit)[sure].all()
+            else:
+                assert bool(((now.double() - want).abs() <= 2 * bound + 2.0 ** -8 * want.abs()).all())
+            if bits == 32:
+                assert bool(((s["exp_avg"].double().reshape(-1) - m).abs() <= 6 * 2.0 ** -24 * (0.9 * m0.abs() + 0.1 * g.abs()) + 1e-40).all())
+                assert bool(((s["exp_avg_sq"].double().reshape(-1) - v).abs() <= 6 * 2.0 ** -24 * v + 1e-40).all())
+            else:
+                block = torch.arange(n, device=cuda_device) // BLOCK
+                for x, k in ((m, "exp_avg"), (v.sqrt(), "exp_avg_root")):
+                    scale = s[k + "_scale"].double()[block]
+                    off = 6 * 2.0 ** -24 * (0.9 * m0.abs() + 0.1 * g.abs())
+                    assert bool(((s[k].double().reshape(-1) * scale - x).abs() <= torch.maximum(x.abs() / 8, scale * 2.0 ** -9) * (1 + 1e-5) + 9 / 8 * off).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("bits", [8, 32])
+def test_what_lies_beside_a_parameter_stays(cuda_device, dtype, bits):
+    flat = torch.randn(4003, device=cuda_device).to(dtype)
+    spans = [(1, 1000), (1003, 1004), (1024, 1024 + 256), (2001, 4000)]
+    kept = flat.clone()
+    params = [torch.nn.Parameter(flat[a:b]) for a, b in spans]
+    opt = dropit.DropITAdamW(params, lr=1e-1, state_bits=bits)
+    for p in params:
+        p.grad = torch.ones_like(p)
+    opt.step()
+    inside = torch.zeros(4003, dtype=torch.bool, device=cuda_device)
+    for a, b in spans:
+        inside[a:b] = True
+    assert torch.equal(flat[~inside], kept[~inside]) and not bool((flat[inside] == kept[inside]).any())
