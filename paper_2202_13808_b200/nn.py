@@ -206,8 +206,7 @@ class DropITGatedLinear(nn.Module):
                  fmt: str = "bitmask", device=None, dtype=None):
         super().__init__()
         self.in_features, self.hidden_features = int(in_features), int(hidden_features)
-        self._gate = api._gate_code(gate)
-        self._fmt = api._FMT_CODE[fmt]
+        api._gate_code(gate), api._FMT_CODE[fmt]        # an error here rather than at the first call
         self.gate, self.gamma, self.fmt = gate, float(gamma), fmt
         self.weight = nn.Parameter(torch.empty(2 * self.hidden_features, self.in_features, device=device, dtype=dtype))
         self.bias = nn.Parameter(torch.empty(2 * self.hidden_features, device=device, dtype=dtype)) if bias else None
@@ -225,7 +224,7 @@ class DropITGatedLinear(nn.Module):
             self.in_features, self.hidden_features, self.bias is not None, self.gate, self.gamma)
 
     def forward(self, x):
-        weight, bias = self.weight, self.bias
+        weight, bias, gate = self.weight, self.bias, api._gate_code(self.gate)
         if torch.is_autocast_enabled("cuda"):      # the type that a Linear would run in
             dt = torch.get_autocast_dtype("cuda")
             x, weight, bias = x.to(dt), weight.to(dt), None if bias is None else bias.to(dt)
@@ -236,8 +235,8 @@ class DropITGatedLinear(nn.Module):
                 # derivatives outside of training are those of the stock operations (Sec. 3.5: inference is unchanged)
                 a, u = F.linear(x, weight, bias).chunk(2, -1)
                 return {"silu": F.silu, "gelu": F.gelu, "relu": F.relu}[self.gate](a) * u
-            return native.gated_linear(x, weight, bias, self._gate, False)[0]
-        return api._native().gated_layer(x, weight, bias, self.gamma, self._fmt, self._gate)
+            return native.gated_linear(x, weight, bias, gate, False)[0]
+        return api._native().gated_layer(x, weight, bias, self.gamma, api._FMT_CODE[self.fmt], gate)
 
 
 class DropITRotary(nn.Module):
