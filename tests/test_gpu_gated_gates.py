@@ -41,3 +41,29 @@ def test_attributes_are_read_at_the_call(cuda_device, training):
     layer.fmt = "dense"
     with pytest.raises((KeyError, ValueError)):
         layer(x)
+
+
+@pytest.mark.parametrize("M", [8, 300])
+@pytest.mark.parametrize("span", [(-12.5, -3.0), (-3.0, 3.0), (3.0, 200.0)])
+def test_gelu_is_accurate_relative_to_its_value(cuda_device, M, span):
+    """Every bf16 of the span, as a with u = 1: one rounding of a value that is off by 2^-12 of itself at most, in the tail too."""
+    H = 64
+    bits = torch.arange(2 ** 16, dtype=torch.int32).to(torch.int16).view(torch.bfloat16).float()
+    a = bits[(bits >= span[0]) & (bits <= span[1])].to(cuda_device)
+    a = a[a.abs() >= 2.0 ** -100]
+    for start in range(0, a.numel(), M * H):
+        part = torch.ones(M * H, device=cuda_device)
+        part[:min(M * H, a.numel() - start)] = a[start:start + M * H]
+        part = part.view(M, H)
+        x = torch.cat([part, torch.ones_like(part)], 1).bfloat16()
+        w = torch.eye(2 * H, device=cuda_device).bfloat16()
+        h, gu = dropit.dropit_gated_linear(x, w, None, "gelu", keep=True)
+        want = _gelu64(part.double())
+        assert bool(((h.double() - want).abs() <= (U + 2.0 ** -12) * want.abs()).all())
+        # du = dh f(a) with dh = 1
+        dgu = dropit.dropit_gated_linear_backward(torch.ones_like(h), gu, "gelu")
+        assert bool(((dgu[:, H:].double() - want).abs() <= (U + 2.0 ** -12) * want.abs()).all())
+        # f' = Phi + a phi passes through zero at -0.7518; elsewhere its terms do not cancel beyond a digit or two
+        slope = 0.5 * torch.special.erfc(-part.double() / 2 ** 0.5) + part.double() * torch.exp(-part.double() ** 2 / 2) / (2 * torch.pi) ** 0.5
+        terms = 0.5 * torch.special.erfc(-part.double() / 2 ** 0.5) + part.double().abs() * torch.exp(-part.double() ** 2 / 2) / (2 * torch.pi) ** 0.5
+        assert bool(((dgu[:, :H].double() - slope).abs() <= U * slope.abs() + 2.0 ** -12 * terms).all())
