@@ -392,6 +392,7 @@ def dropit_rotary(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.T
                   in_place: bool = False):
     """Queries and, unless None, keys turned by their positions: (q', k').  q [batch, length, heads, head_dim] or [length, heads, head_dim],
     bf16 or fp32, any strides as long as the channels of a head lie together; k the same with heads of its own.  positions
-    [length, axes] or [batch, length, axes], int32, int64 or fp32.  Results are contiguous, or written over q and k with in_place.
+    [length, axes] or [batch, length, axes], int32, int64 or fp32.  Results are contiguous, or written over q and k with in_place, where
+    no two heads of them may have channels in common.
     No autograd: that is nn.DropITRotary."""
     return _native().rotary(q, k, positions, plan, bool(inverse), bool(in_place))

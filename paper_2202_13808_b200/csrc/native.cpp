@@ -9,8 +9,8 @@
 #include <torch/csrc/autograd/functions/utils.h>
 #include <torch/csrc/autograd/saved_variable.h>
 #include <torch/extension.h>
-#include <ATen/MemoryOverlap.h>
 
+#include <algorithm>
 #include <cstdlib>
 #include <mutex>
 #include <tuple>
@@ -488,27 +488,69 @@ dropit_rotary_tensor rotary_tensor(const Tensor& in, Tensor& out, const dropit_r
 }
 Tensor rotary_input(const Tensor& t) { return t.dim() && t.stride(-1) != 1 ? t.contiguous() : t; }
 
-// Whether slices along the heads of one projection have channels in common.
-bool share_channels(const Tensor& q, const Tensor& k) {
-    if (q.numel() == 0 || k.numel() == 0 || q.dim() < 3 || k.dim() != q.dim() || !q.storage().is_alias_of(k.storage())) return false;
-    const int64_t off = k.storage_offset() - q.storage_offset();
-    for (int64_t h = 1 - k.size(-2); h < q.size(-2); ++h)          // heads of q less heads of k
-        if (std::abs(off - h * q.stride(-2)) < q.size(-1)) return true;
+// Writing in place: do two (token, head)s have channels in common?  Rows of `size(-1)` channels lie at multiples of the other dimensions' strides.
+// Of one tensor: no, if every stride passes all that the smaller ones reach (any permutation of a slice of a dense tensor).
+bool has_places_of_its_own(const Tensor& t) {
+    std::vector<std::pair<int64_t, int64_t>> dims;
+    for (int64_t d = 0; d + 1 < t.dim(); ++d)
+        if (t.size(d) > 1) dims.emplace_back(t.stride(d), t.size(d));
+    std::sort(dims.begin(), dims.end());
+    int64_t reach = t.dim() ? t.size(-1) : 1;
+    for (const auto& [stride, size] : dims) {
+        if (stride < reach) return t.numel() == 0;
+        reach += (size - 1) * stride;
+    }
+    return true;
+}
+// Of two: is there a choice of steps whose sum comes within a row's width of the distance between the tensors?  A dimension that both have with the
+// same stride counts once, by the difference of its indices.  Larger strides first: what the smaller ones reach leaves one to three choices for each.
+struct Steps {
+    int64_t stride, low, high;
+};
+bool meets(const std::vector<Steps>& steps, const std::vector<int64_t>& reach, size_t at, int64_t left, int& tries) {
+    if (--tries < 0) return true;                                   // strides that are not worth the search
+    if (at == steps.size()) return std::abs(left) <= reach[at];
+    const Steps& s = steps[at];
+    const auto quotient = [&](int64_t n) { return n / s.stride - (n % s.stride < 0); };     // rounded down
+    const int64_t first = std::max(s.low, quotient(left - reach[at + 1] + s.stride - 1)), last = std::min(s.high, quotient(left + reach[at + 1]));
+    for (int64_t i = first; i <= last; ++i)
+        if (meets(steps, reach, at + 1, left - i * s.stride, tries)) return true;
     return false;
+}
+bool share_channels(const Tensor& q, const Tensor& k) {
+    if (q.numel() == 0 || k.numel() == 0 || q.scalar_type() != k.scalar_type()) return false;
+    const int64_t size = q.element_size(), bytes = (const char*)k.data_ptr() - (const char*)q.data_ptr();
+    std::vector<Steps> steps;
+    for (int64_t d = 0; d + 1 < q.dim(); ++d)
+        if (q.size(d) > 1) steps.push_back({q.stride(d), 0, q.size(d) - 1});
+    for (int64_t d = 0; d + 1 < k.dim(); ++d) {
+        if (k.size(d) <= 1) continue;
+        auto same = std::find_if(steps.begin(), steps.end(), [&](const Steps& s) { return s.stride == k.stride(d) && s.low == 0; });
+        if (same != steps.end()) same->low = 1 - k.size(d);
+        else steps.push_back({k.stride(d), 1 - k.size(d), 0});
+    }
+    std::sort(steps.begin(), steps.end(), [](const Steps& a, const Steps& b) { return a.stride > b.stride; });
+    std::vector<int64_t> reach(steps.size() + 1);
+    reach[steps.size()] = std::max(q.size(-1), k.size(-1)) - 1;
+    for (size_t i = steps.size(); i-- > 0;) reach[i] = reach[i + 1] + std::max(-steps[i].low, steps[i].high) * steps[i].stride;
+    int tries = 1 << 14;
+    return meets(steps, reach, 0, bytes / size, tries);             // (both are aligned to their values)
 }
 
 std::tuple<Tensor, c10::optional<Tensor>> rotary(const Tensor& q_in, const c10::optional<Tensor>& k_in, const Tensor& positions, const Tensor& plan_bytes,
                                                  bool inverse, bool in_place) {
     refuse_tangents({q_in, k_in, positions}, "the rotation");
     const dropit_rotary_plan* plan = plan_of(plan_bytes);
+    const bool has_k = k_in.has_value() && k_in->defined();
+    if (in_place) {
+        for (const Tensor& t : {q_in, has_k ? *k_in : q_in}) {
+            if (t.dim() && t.stride(-1) != 1) throw py::value_error("in place: the channels of a head must lie together");
+            if (!has_places_of_its_own(t)) throw py::value_error("in place: every head of a token must have a place of its own");
+        }
+        if (has_k && share_channels(q_in, *k_in)) throw py::value_error("in place: q and k share values");
+    }
     if (!q_in.is_cuda()) throw py::value_error("q must be a CUDA tensor (there is no CPU path)");
     const dropit_dtype dt = dtype_code(q_in, "q");
-    const bool has_k = k_in.has_value() && k_in->defined();
-    if (in_place && ((q_in.dim() && q_in.stride(-1) != 1) || (has_k && k_in->dim() && k_in->stride(-1) != 1)))
-        throw py::value_error("in place: the channels of a head must lie together");
-    if (in_place && (at::has_internal_overlap(q_in) == at::MemOverlap::Yes || (has_k && at::has_internal_overlap(*k_in) == at::MemOverlap::Yes)))
-        throw py::value_error("in place: an expanded tensor has no place of its own");
-    if (in_place && has_k && share_channels(q_in, *k_in)) throw py::value_error("in place: q and k share values");
     const Tensor q = rotary_input(q_in), k = has_k ? rotary_input(*k_in) : Tensor();
     c10::cuda::CUDAGuard guard(q.device());
     Tensor q_out = in_place ? q : Tensor(at::detail::empty_cuda(q.sizes(), q.scalar_type(), q.device(), c10::nullopt)), k_out;
