@@ -548,6 +548,9 @@ std::tuple<Tensor, c10::optional<Tensor>> rotary(const Tensor& q_in, const c10::
             if (!has_places_of_its_own(t)) throw py::value_error("in place: every head of a token must have a place of its own");
         }
         if (has_k && share_channels(q_in, *k_in)) throw py::value_error("in place: q and k share values");
+        // what is written over would pass for the result of the operation that q and k came from
+        TORCH_CHECK(!at::GradMode::is_enabled() || !(q_in.requires_grad() || (has_k && k_in->requires_grad())),
+                    "in place: q or k requires a gradient, which the rotation would not be part of");
     }
     if (!q_in.is_cuda()) throw py::value_error("q must be a CUDA tensor (there is no CPU path)");
     const dropit_dtype dt = dtype_code(q_in, "q");
@@ -618,6 +621,7 @@ std::tuple<Tensor, c10::optional<Tensor>> rotary_layer(const Tensor& q, const c1
                                                        bool inverse) {
     const bool has_k = k.has_value() && k->defined();
     const Tensor key = has_k ? *k : Tensor();
+    TORCH_CHECK(!at::GradMode::is_enabled() || !positions.requires_grad(), "positions require a gradient, which the rotation does not have");
     if (!at::GradMode::is_enabled() || !(wants(q) || wants(key))) return rotary(q, k, positions, plan, inverse, false);
     Tensor q_out;
     c10::optional<Tensor> k_out;

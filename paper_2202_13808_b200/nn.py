@@ -241,7 +241,8 @@ class DropITGatedLinear(nn.Module):
 
 class DropITRotary(nn.Module):
     """Rotary positions with several axes on queries and keys (see api.dropit_rotary and dropit_rotary_plan): (q, k, positions) ->
-    (q', k').  The backward pass is the inverse rotation and keeps the positions only; forward-mode derivatives are refused."""
+    (q', k').  The backward pass is the inverse rotation and keeps the positions only; forward-mode derivatives and
+    positions that require a gradient are refused."""
 
     def __init__(self, head_dim: int, sections, theta: float = 10000.0, interleaved: bool = False, shared: bool = False):
         super().__init__()

@@ -95,6 +95,24 @@ def test_a_view_that_meets_itself():
             _call(_buffer(*size), _buffer(1024).as_strided(size, stride), in_place=True)
 
 
+def test_gradients_that_would_be_lost():
+    q, k, at = torch.zeros(1, 4, 2, D, requires_grad=True), torch.zeros(1, 4, 2, D), torch.zeros(4, 1)
+    for a, b in ((q, k), (k, q), (q * 1, None)):
+        with pytest.raises(RuntimeError, match="gradient"):
+            _call(a, b, in_place=True)
+    with torch.no_grad(), pytest.raises(ValueError, match="CUDA tensor"):
+        _call(q, k, in_place=True)
+    with pytest.raises(ValueError, match="CUDA tensor"):
+        _call(q, k)
+    # fp32 positions are values that a model could learn, but the rotation has no gradient for them
+    rot, at = dropit.DropITRotary(D, (D,)), at.requires_grad_(True)
+    for f in (lambda: rot(q, k, at), lambda: rot(k, None, at)):
+        with pytest.raises(RuntimeError, match="positions"):
+            f()
+    with torch.no_grad(), pytest.raises(ValueError, match="CUDA tensor"):
+        rot(q, k, at)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("how", sorted(APART))
 def test_in_place_is_what_the_copy_is(cuda_device, how):
