@@ -67,3 +67,35 @@ def test_gelu_is_accurate_relative_to_its_value(cuda_device, M, span):
         slope = 0.5 * torch.special.erfc(-part.double() / 2 ** 0.5) + part.double() * torch.exp(-part.double() ** 2 / 2) / (2 * torch.pi) ** 0.5
         terms = 0.5 * torch.special.erfc(-part.double() / 2 ** 0.5) + part.double().abs() * torch.exp(-part.double() ** 2 / 2) / (2 * torch.pi) ** 0.5
         assert bool(((dgu[:, :H].double() - slope).abs() <= U * slope.abs() + 2.0 ** -12 * terms).all())
+
+
+def _kernel_nodes(graph):
+    runtime = ctypes.CDLL("libcudart.so.12")
+    count = ctypes.c_size_t(0)
+    assert runtime.cudaGraphGetNodes(ctypes.c_void_p(graph.raw_cuda_graph()), None, ctypes.byref(count)) == 0
+    return count.value
+
+
+def test_rows_behind_the_full_waves_whose_tiles_share_a_long_axis(cuda_device):
+    """Where the last wave is nearly empty its rows are a launch of their own; their summed axis of 4096 is long enough for the clusters of two and
+    four pairs that a few tiles get, which then begin at another row."""
+    C, H = 256, 2048
+    g = torch.Generator(device=cuda_device).manual_seed(1)
+    w = (torch.randn(2 * H, C, generator=g, device=cuda_device) * C ** -0.5).bfloat16()
+    pairs, split = torch.cuda.get_device_properties(cuda_device).multi_processor_count // 2, 0
+    for tiles_over in (1, 2, 4):
+        for less in range(0, 5):                # some SMs may have no partner
+            M = 256 * (pairs - less + tiles_over) - 37
+            dgu = torch.randn(M, 2 * H, generator=g, device=cuda_device).bfloat16()
+            dx = dropit.dropit_gated_input_grad(dgu, w)
+            want, size = dgu.double() @ w.double(), dgu.double().abs() @ w.double().abs()
+            bound = 2 * H * 2.0 ** -24 * size
+            assert bool(((dx.double() - want).abs() <= bound + U * (want.abs() + bound)).all())
+            graph = torch.cuda.CUDAGraph(keep_graph=True)
+            with torch.cuda.graph(graph):
+                again = dropit.dropit_gated_input_grad(dgu, w)
+            split += _kernel_nodes(graph) == 2
+            graph.replay()
+            assert torch.equal(again, dx)
+    dropit.check_device_status(cuda_device)
+    assert split
