@@ -226,6 +226,8 @@ gated_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Shape
                         break;
                     }
                     const uint32_t bar = full0 + 8u * s;
+                    // in front of the copies: the slot's next round is another thread's, which waits for what these bring
+                    reinterpret_cast<volatile int*>(ctl->issued)[s] = (int)round + 1;
                     if (!member) ptx::mbar_arrive_expect_tx(&ctl->full[s], 2u * kStageTx);
                     uint8_t* a = left + s * kLeftBytes;
                     uint8_t* b = right + s * kRightBytes;
@@ -252,7 +254,6 @@ gated_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Shape
                                 ptx::tma_load_2d_pair(b + g * (64 * kStep * 2), &maps.right, n0 + member * kHidden + 64 * g, k0, bar);
                         }
                     }
-                    reinterpret_cast<volatile int*>(ctl->issued)[s] = (int)round + 1;
                 }
                 k -= steps;
             }
