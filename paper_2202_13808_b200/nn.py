@@ -230,9 +230,10 @@ class DropITGatedLinear(nn.Module):
             x, weight, bias = x.to(dt), weight.to(dt), None if bias is None else bias.to(dt)
         if not (self.training and torch.is_grad_enabled()):
             native = api._native()
-            if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or (bias is not None and bias.requires_grad)) or \
+            if not (x.is_cuda and x.dtype in (torch.bfloat16, torch.float32)) or \
+                    torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or (bias is not None and bias.requires_grad)) or \
                     native.has_tangent(x) or native.has_tangent(weight) or native.has_tangent(bias):
-                # derivatives outside of training are those of the stock operations (Sec. 3.5: inference is unchanged)
+                # outside of training, derivatives and what the kernels do not take are those of the stock operations (Sec. 3.5: inference is unchanged)
                 a, u = F.linear(x, weight, bias).chunk(2, -1)
                 return {"silu": F.silu, "gelu": F.gelu, "relu": F.relu}[self.gate](a) * u
             return native.gated_linear(x, weight, bias, gate, False)[0]
