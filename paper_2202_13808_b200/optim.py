@@ -206,11 +206,11 @@ class DropITAdamW(torch.optim.Optimizer):
 
     def step(self, closure=None, grad_factor=None):
         if self._optimizer_step_pre_hooks or self._optimizer_step_post_hooks or _optimizer._global_optimizer_pre_hooks or \
-                _optimizer._global_optimizer_post_hooks:
+                _optimizer._global_optimizer_post_hooks or torch.autograd._profiler_enabled():
             return _hooked_step(self, closure, grad_factor)
         return self._step(closure, grad_factor)
 
-    step.hooked = True      # the base class would wrap it for hooks and a profiler's label: 10 us a call, twice what a small step takes
+    step.hooked = True      # the base class would wrap every call for hooks and a profiler's label: 10 us, twice what a small step takes
 
     def _step(self, closure=None, grad_factor=None):
         loss = None
