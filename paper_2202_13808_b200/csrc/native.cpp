@@ -243,10 +243,11 @@ Tensor gelu_linear(const Tensor& x, const Tensor& weight, const c10::optional<Te
 }
 
 // The nodes below compute no forward-mode derivatives, and results without a tangent would pass for constants.
-bool has_tangent(const c10::optional<Tensor>& t) { return t.has_value() && t->defined() && t->_fw_grad(/*level=*/0).defined(); }
-void refuse_tangents(std::initializer_list<c10::optional<Tensor>> inputs, const char* name) {
-    for (const auto& t : inputs)
-        TORCH_CHECK_NOT_IMPLEMENTED(!has_tangent(t), name, " has no forward-mode derivative");
+bool has_tangent(const Tensor& t) { return t.defined() && t._fw_grad(/*level=*/0).defined(); }
+bool has_tangent(const c10::optional<Tensor>& t) { return t.has_value() && has_tangent(*t); }
+template <typename... T>
+void refuse_tangents(const char* name, const T&... inputs) {
+    TORCH_CHECK_NOT_IMPLEMENTED(!(has_tangent(inputs) || ...), name, " has no forward-mode derivative");
 }
 
 // ---- gated linear: h = f(x Wg^T + bg) * (x Wu^T + bu) ----
@@ -266,7 +267,6 @@ struct GatedSizes {
     dropit_dtype dtype;
 };
 GatedSizes gated_sizes(const Tensor& x, const Tensor& weight, const c10::optional<Tensor>& bias) {
-    refuse_tangents({x, weight, bias}, "the gated linear");
     if (!x.is_cuda()) throw py::value_error("x must be a CUDA tensor (there is no CPU path)");
     GatedSizes s;
     s.dtype = dtype_code(x, "x");
@@ -304,6 +304,7 @@ std::tuple<Tensor, Tensor> gated_products(const Tensor& x, const Tensor& weight,
 }
 
 std::tuple<Tensor, c10::optional<Tensor>> gated_linear(const Tensor& x, const Tensor& weight, const c10::optional<Tensor>& bias, int64_t gate, bool keep) {
+    refuse_tangents("the gated linear", x, weight, bias);
     const GatedSizes s = gated_sizes(x, weight, bias);
     Tensor h, gu;
     std::tie(h, gu) = gated_products(aligned(x), weight, bias, s, gate, keep);
@@ -312,8 +313,16 @@ std::tuple<Tensor, c10::optional<Tensor>> gated_linear(const Tensor& x, const Te
     return {h, kept};
 }
 
+// h outside of training, unless a derivative is asked for or the kernels have no form for x: nothing then.
+c10::optional<Tensor> gated_inference(const Tensor& x, const Tensor& weight, const c10::optional<Tensor>& bias, int64_t gate) {
+    if (!x.is_cuda() || (x.scalar_type() != at::kBFloat16 && x.scalar_type() != at::kFloat)) return c10::nullopt;
+    if (at::GradMode::is_enabled() && (x.requires_grad() || weight.requires_grad() || (bias.has_value() && bias->requires_grad()))) return c10::nullopt;
+    if (has_tangent(x) || has_tangent(weight) || has_tangent(bias)) return c10::nullopt;
+    return std::get<0>(gated_products(aligned(x), weight, bias, gated_sizes(x, weight, bias), gate, false));
+}
+
 std::tuple<Tensor, c10::optional<Tensor>> gated_linear_backward(const Tensor& dh, const Tensor& gu, int64_t gate, bool want_db) {
-    refuse_tangents({dh, gu}, "the gated linear's gradient");
+    refuse_tangents("the gated linear's gradient", dh, gu);
     if (!dh.is_cuda()) throw py::value_error("dh must be a CUDA tensor (there is no CPU path)");
     const dropit_dtype dt = dtype_code(dh, "dh");
     require_like(gu, dh, "gu", "dh");
@@ -337,7 +346,7 @@ std::tuple<Tensor, c10::optional<Tensor>> gated_linear_backward(const Tensor& dh
 }
 
 Tensor gated_input_grad(const Tensor& dgu, const Tensor& weight) {
-    refuse_tangents({dgu, weight}, "the gated linear's gradient");
+    refuse_tangents("the gated linear's gradient", dgu, weight);
     if (!dgu.is_cuda()) throw py::value_error("dgu must be a CUDA tensor (there is no CPU path)");
     const dropit_dtype dt = dtype_code(dgu, "dgu");
     require_like(weight, dgu, "weight", "dgu");
@@ -375,7 +384,7 @@ struct GatedLinearNode : public torch::autograd::Node {
         std::lock_guard<std::mutex> lock(mutex_);
         torch::autograd::variable_list out(3);
         if (!grads[0].defined()) return out;
-        refuse_tangents({grads[0]}, "the gated linear's gradient");
+        refuse_tangents("the gated linear's gradient", grads[0]);
         const Tensor weight = weight_.unpack(), gu = gu_.unpack();          // an error, if they have been released
         const bool want_x = task_should_compute_output(0), want_w = task_should_compute_output(1), want_b = task_should_compute_output(2);
         {
@@ -422,6 +431,7 @@ struct GatedLinearNode : public torch::autograd::Node {
     }
 };
 Tensor gated_layer(const Tensor& x, const Tensor& weight, const c10::optional<Tensor>& bias, double gamma, int64_t fmt, int64_t gate) {
+    refuse_tangents("the gated linear", x, weight, bias);
     const Tensor b = bias.has_value() ? *bias : Tensor();
     const GatedSizes s = gated_sizes(x, weight, bias);
     const bool records = at::GradMode::is_enabled() && (wants(x) || wants(weight) || wants(b));
@@ -539,7 +549,7 @@ bool share_channels(const Tensor& q, const Tensor& k) {
 
 std::tuple<Tensor, c10::optional<Tensor>> rotary(const Tensor& q_in, const c10::optional<Tensor>& k_in, const Tensor& positions, const Tensor& plan_bytes,
                                                  bool inverse, bool in_place) {
-    refuse_tangents({q_in, k_in, positions}, "the rotation");
+    refuse_tangents("the rotation", q_in, k_in, positions);
     const dropit_rotary_plan* plan = plan_of(plan_bytes);
     const bool has_k = k_in.has_value() && k_in->defined();
     if (in_place) {
@@ -724,8 +734,8 @@ PYBIND11_MODULE(_native, m) {
     m.def("weight_grad", torch::wrap_pybind_function_no_gil(weight_grad));
     m.def("conv_weight_grad", torch::wrap_pybind_function_no_gil(conv_weight_grad));
     m.def("gelu_linear", torch::wrap_pybind_function_no_gil(gelu_linear));
-    m.def("has_tangent", has_tangent);
     m.def("gated_linear", torch::wrap_pybind_function_no_gil(gated_linear));
+    m.def("gated_inference", torch::wrap_pybind_function_no_gil(gated_inference));
     m.def("gated_linear_backward", torch::wrap_pybind_function_no_gil(gated_linear_backward));
     m.def("gated_input_grad", torch::wrap_pybind_function_no_gil(gated_input_grad));
     m.def("gated_layer", torch::wrap_pybind_function_no_gil(gated_layer));

@@ -292,8 +292,9 @@ extern "C" dropit_status dropit_rotary(const dropit_rotary_plan* plan, int64_t b
     if (!plan || !q || batch < 0 || length < 0 || length > INT32_MAX) return DROPIT_ERR_INVALID_ARG;
     if (plan->pairs < 1 || plan->pairs > DROPIT_ROTARY_MAX_PAIRS || plan->head_dim < 2 * plan->pairs) return DROPIT_ERR_INVALID_ARG;
     if (plan->axes < 1 || plan->axes > DROPIT_ROTARY_MAX_AXES) return DROPIT_ERR_INVALID_ARG;
-    for (int j = 0; j < plan->pairs; ++j)               // positions are read by it
-        if (plan->axis[j] >= plan->axes) return DROPIT_ERR_INVALID_ARG;
+    uint8_t last_axis = 0;                              // positions are read by them
+    for (int j = 0; j < plan->pairs; ++j) last_axis = std::max(last_axis, plan->axis[j]);
+    if (last_axis >= plan->axes) return DROPIT_ERR_INVALID_ARG;
     if (dtype != DROPIT_BF16 && dtype != DROPIT_F32) return DROPIT_ERR_INVALID_ARG;
     if (position_type != DROPIT_POSITION_I32 && position_type != DROPIT_POSITION_I64 && position_type != DROPIT_POSITION_F32)
         return DROPIT_ERR_INVALID_ARG;

@@ -224,19 +224,19 @@ class DropITGatedLinear(nn.Module):
             self.in_features, self.hidden_features, self.bias is not None, self.gate, self.gamma)
 
     def forward(self, x):
-        weight, bias, gate = self.weight, self.bias, api._gate_code(self.gate)
+        weight, bias, gate = self.weight, self.bias, api._GATE.get(self.gate)
+        if gate is None:
+            api._gate_code(self.gate)       # raises
         if torch.is_autocast_enabled("cuda"):      # the type that a Linear would run in
             dt = torch.get_autocast_dtype("cuda")
             x, weight, bias = x.to(dt), weight.to(dt), None if bias is None else bias.to(dt)
         if not (self.training and torch.is_grad_enabled()):
-            native = api._native()
-            if not (x.is_cuda and x.dtype in (torch.bfloat16, torch.float32)) or \
-                    torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or (bias is not None and bias.requires_grad)) or \
-                    native.has_tangent(x) or native.has_tangent(weight) or native.has_tangent(bias):
-                # outside of training, derivatives and what the kernels do not take are those of the stock operations (Sec. 3.5: inference is unchanged)
-                a, u = F.linear(x, weight, bias).chunk(2, -1)
-                return {"silu": F.silu, "gelu": F.gelu, "relu": F.relu}[self.gate](a) * u
-            return native.gated_linear(x, weight, bias, gate, False)[0]
+            h = api._native().gated_inference(x, weight, bias, gate)
+            if h is not None:
+                return h
+            # outside of training, derivatives and what the kernels do not take are those of the stock operations (Sec. 3.5: inference is unchanged)
+            a, u = F.linear(x, weight, bias).chunk(2, -1)
+            return {"silu": F.silu, "gelu": F.gelu, "relu": F.relu}[self.gate](a) * u
         return api._native().gated_layer(x, weight, bias, self.gamma, api._FMT_CODE[self.fmt], gate)
 
 

@@ -10,6 +10,7 @@ from torch.optim import optimizer as _optimizer
 
 from . import api
 
+_profiler_enabled = torch.autograd._profiler_enabled
 BLOCK = 256         # values that share one scale where moments are held in 8 bits; every tensor begins on a block of its own
 
 
@@ -206,7 +207,7 @@ class DropITAdamW(torch.optim.Optimizer):
 
     def step(self, closure=None, grad_factor=None):
         if self._optimizer_step_pre_hooks or self._optimizer_step_post_hooks or _optimizer._global_optimizer_pre_hooks or \
-                _optimizer._global_optimizer_post_hooks or torch.autograd._profiler_enabled():
+                _optimizer._global_optimizer_post_hooks or _profiler_enabled():
             return _hooked_step(self, closure, grad_factor)
         return self._step(closure, grad_factor)
 
@@ -230,7 +231,8 @@ class DropITAdamW(torch.optim.Optimizer):
             self._plan, settings, self.state_bits, self.dither, self.seed, a["exp_avg"], a["exp_avg_root" if self.state_bits == 8 else "exp_avg_sq"],
             a.get("exp_avg_scale"), a.get("exp_avg_root_scale"), a.get("master"), self._steps, self._ticket,
             None if grad_factor is None else self._scalar(grad_factor, "grad_factor"))
-        self._captured |= captured
+        if captured:
+            self._captured = True
         return loss
 
     def _scalar(self, t, name):
