@@ -589,12 +589,12 @@ std::tuple<Tensor, c10::optional<Tensor>> rotary(const Tensor& q_in, const c10::
         throw py::value_error("positions must be [length, " + std::to_string(plan->axes) + "] or [batch, length, " + std::to_string(plan->axes) +
                               "] with q's length and batch");
     const int64_t pos_batch = each && positions.size(0) != 1 ? positions.stride(0) : 0;
-    check(dropit_rotary(plan, batch, length, &tq, has_k ? &tk : nullptr, positions.numel() ? positions.data_ptr() : nullptr, type, pos_batch,
-                        positions.stride(-2), positions.stride(-1), dt, inverse, current_stream(q)), "dropit_rotary");
-    if (in_place) {
+    if (in_place) {         // an error for tensors of inference mode outside of it, before they change
         q_out.unsafeGetTensorImpl()->bump_version();
         if (has_k) k_out.unsafeGetTensorImpl()->bump_version();
     }
+    check(dropit_rotary(plan, batch, length, &tq, has_k ? &tk : nullptr, positions.numel() ? positions.data_ptr() : nullptr, type, pos_batch,
+                        positions.stride(-2), positions.stride(-1), dt, inverse, current_stream(q)), "dropit_rotary");
     c10::optional<Tensor> second;
     if (has_k) second = k_out;
     return {q_out, second};
@@ -704,14 +704,14 @@ bool adamw_step(const AdamWParams& all, const std::vector<AdamWGroupTuple>& sett
                                  all.first_block[i], (int32_t)i, (float)lr, (float)decay});
     }
     auto words = [](const c10::optional<Tensor>& t) { return t.has_value() ? t->data_ptr<float>() : nullptr; };
+    for (size_t i = 0; i < all.params.size(); ++i)          // autograd sees that they change
+        if (all.params[i].grad().defined()) all.params[i].unsafeGetTensorImpl()->bump_version();
     for (Call& c : calls) {
         const dropit_adamw_state state = {exp_avg.data_ptr(), exp_avg_sq.data_ptr(), words(exp_avg_scale), words(exp_avg_sq_scale),
                                           c.options.param_dtype == DROPIT_BF16 ? words(master) : nullptr, steps.data_ptr<int32_t>(),
                                           (uint32_t*)ticket.data_ptr(), words(grad_factor)};
         check(dropit_adamw_step(c.tensors.data(), (int)c.tensors.size(), &c.options, &state, current_stream(exp_avg)), "dropit_adamw_step");
     }
-    for (size_t i = 0; i < all.params.size(); ++i)
-        if (all.params[i].grad().defined()) all.params[i].unsafeGetTensorImpl()->bump_version();
     return !calls.empty() && c10::cuda::currentStreamCaptureStatusMayInitCtx() != c10::cuda::CaptureStatus::None;
 }
 
