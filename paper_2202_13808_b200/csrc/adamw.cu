@@ -30,8 +30,8 @@ namespace {
 constexpr int kBlock = DROPIT_ADAMW_BLOCK;
 constexpr int kThreads = 128;
 constexpr int kMaxEntries = 512;
-constexpr uint32_t kMaxRun = 16;                    // blocks of a run (8 bits 213 / 205 / 202 us with 8 / 16 / 32)
-constexpr int kResident8 = 5, kResident32 = 4;          // CTAs per SM: 8 bits 216 / 205 / 227 us with 4 / 5 / 6, which spills
+constexpr uint32_t kMaxRun = 16;                    // blocks of a run (8 bits, 86.6 M values: 315 / 225 / 217 / 211 us with 1 / 8 / 16 / 32; at other sizes 16 and 32 take turns)
+constexpr int kResident8 = 5, kResident32 = 4;          // CTAs per SM: 8 bits 219 / 217 / 231 us with 4 / 5 / 6, which spills
 
 struct Entry {
     void* p;
@@ -401,8 +401,8 @@ __device__ __forceinline__ void write(const Args& a, const Step& k, uint32_t ins
 
 // Warps take runs of a tensor's blocks in turn (a.run of them, fewer where that leaves warps without any), so that the tensor's constants are
 // looked up and the scales of a run come and go once; the next block's loads are under way while one is rounded and written.
-// 85 M bf16 values with moments in 8 bits: 205 us; 268 with single blocks dealt out (nearly every one another tensor's), 295 with one stretch of
-// blocks a CTA, whose streams keep in step.
+// 86.6 M bf16 values with moments in 8 bits: 217 us; 315 with single blocks dealt out (nearly every one another tensor's).  One stretch of blocks a CTA,
+// whose streams keep in step, took 295 where this form took 205 (before its roots were exact).
 template <typename P, typename G, bool BITS8, int FORM>
 __global__ void __launch_bounds__(kThreads, BITS8 ? kResident8 : kResident32)
 adamw_kernel(const __grid_constant__ Args a) {

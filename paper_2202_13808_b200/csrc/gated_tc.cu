@@ -9,8 +9,9 @@
 // Few rows: narrower tiles, so that more SMs take part, and for dx, whose summed axis is 2H long, two or four pairs of a cluster share a tile's
 // summed axis and add their accumulators through the cluster's shared memory, in order (see plan()).
 //
-// Bound by the tensor cores for many rows: 2 M C 2H flops.  12608 x 768 -> 2048 (79 GFLOP): forward 57 us, 75 where a and u are kept, whose stores take the
-// operands' way to L2; dx 66.
+// Bound by the tensor cores for many rows, 2 M C 2H flops, as long as the sum is longer than the epilogue of a tile.  12608 x 768 -> 2048 (79 GFLOP, 48 us
+// at the measured rate): forward 57 us (ReLU 56, GELU 61), 71 where a and u are kept, 73 with a bias; there the epilogue is the limit: at 128 channels, with 8 us of MMAs, it takes
+// 36 and 49 (SiLU).  dx 65 in bursts, 73 for long under the power cap (a library product of its size 58 and 66).
 //
 // Rounded to bf16: h, a, u and dx, each once from its fp32 sum.  a and u in fp32 would double what the layer keeps (103 MB at this size) and
 // the stores that bound it; the gradients carry 0.3 % (rms) instead of 0.17 % for it and for dgu, which the tensor cores take in bf16.
@@ -582,8 +583,9 @@ static dropit_status input_grad_rows(const Plan& p, const uint16_t* dgu, const v
 }
 
 // A last wave of a few tiles takes as long as their whole summed axis.  Where it is a sixteenth of the pairs or less, the rows of the full waves are one
-// launch and the rest, whose pairs share the axis, another: 12608 x 4096 -> 768 (150 tiles on 74 pairs) 66 us, in one launch 69.5.  With more tiles in
-// the last wave a second launch costs more than it saves (32768 rows, 14 tiles: 154 and 151 us; 25000 x 2048 -> 384, 48 tiles: 61 and 53).
+// launch and the rest, whose pairs share the axis, another (us in bursts, one launch in brackets): 12608 x 4096 -> 768 (150 tiles on 74 pairs) 65 (71),
+// 19200 x 4096 -> 256 (75 tiles) 48 (55); with half the sum the second launch costs what it saves, 19000 x 2048 -> 768 (225 tiles) 52 (51).  With more tiles in
+// the last wave it costs more (32768 rows, 14 tiles: 154 and 151; 25000 x 2048 -> 384, 48 tiles: 61 and 53).
 dropit_status gated_tc_input_grad(const void* dgu, const void* w, int64_t M, int64_t C, int64_t H, void* dx, int32_t* dev_status, cudaStream_t stream) {
     const Plan whole = plan(kInputGrad, M, C, 2 * H);
     const uint16_t* from = reinterpret_cast<const uint16_t*>(dgu);
