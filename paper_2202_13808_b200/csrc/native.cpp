@@ -318,7 +318,10 @@ c10::optional<Tensor> gated_inference(const Tensor& x, const Tensor& weight, con
     if (!x.is_cuda() || (x.scalar_type() != at::kBFloat16 && x.scalar_type() != at::kFloat)) return c10::nullopt;
     if (at::GradMode::is_enabled() && (x.requires_grad() || weight.requires_grad() || (bias.has_value() && bias->requires_grad()))) return c10::nullopt;
     if (has_tangent(x) || has_tangent(weight) || has_tangent(bias)) return c10::nullopt;
-    return std::get<0>(gated_products(aligned(x), weight, bias, gated_sizes(x, weight, bias), gate, false));
+    const GatedSizes s = gated_sizes(x, weight, bias);
+    const int64_t limit = (int64_t)1 << 31;
+    if (s.M >= limit || s.M * std::max(s.C, 2 * s.H) >= limit) return c10::nullopt;
+    return std::get<0>(gated_products(aligned(x), weight, bias, s, gate, false));
 }
 
 std::tuple<Tensor, c10::optional<Tensor>> gated_linear_backward(const Tensor& dh, const Tensor& gu, int64_t gate, bool want_db) {

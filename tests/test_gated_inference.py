@@ -48,3 +48,20 @@ def test_no_rows(cuda_device, dtype):
     assert not bool(layer.weight.grad.any()) and not bool(layer.bias.grad.any())
     with torch.no_grad():
         assert layer.eval()(x).shape == (2, 0, 16)
+
+
+@pytest.mark.gpu
+def test_more_values_than_a_call_takes(cuda_device):
+    """2^31 projections and one row more: the library's call is refused, the layer takes the stock operations."""
+    if torch.cuda.mem_get_info(cuda_device)[0] < 20 * 2 ** 30:
+        pytest.skip("needs 20 GB")
+    M = 2 ** 20 + 1
+    layer = dropit.DropITGatedLinear(8, 1024, device=cuda_device, dtype=torch.bfloat16).eval()
+    x = torch.randn(M, 8, device=cuda_device, dtype=torch.bfloat16)
+    with torch.no_grad():
+        with pytest.raises(dropit.DropITError):
+            dropit.dropit_gated_linear(x, layer.weight, layer.bias)
+        h = layer(x)
+        a, u = F.linear(x[-3:], layer.weight, layer.bias).float().chunk(2, -1)
+    # a, u, f(a) and the product each rounded to bf16
+    assert h.shape == (M, 1024) and bool(((h[-3:].float() - F.silu(a) * u).abs() <= 5 * 2.0 ** -8 * (a * u).abs() + 1e-6).all())
