@@ -341,9 +341,11 @@ dropit_status dropit_gated_input_grad(const void* dgu, const void* w, int64_t M,
  *     (one ladder of frequencies dealt out to the axes).  interleaved: pair j = channels (2j, 2j + 1), else (j, j + rotated / 2).  theta >= 1;
  *     up to DROPIT_ROTARY_MAX_PAIRS pairs and DROPIT_ROTARY_MAX_AXES axes.
  *   dropit_rotary: queries and, unless NULL, keys, [batch, length, heads, head_dim] each with strides of its own in elements (the channels of a
- *     head lie together; element-aligned is enough); out may be in with the same strides, any other overlap is not allowed.
+ *     head lie together; element-aligned is enough); out may be in with the same strides, any other overlap is not allowed.  The heads of both times
+ *     head_dim are 2^20 at most.
  *     positions [device], strides in elements (0 repeats).  Whole numbers (32 or 64 bits): the angle is exact to 2^-31 of a turn for |p| < 2^31.
- *     fp32: the product is formed in 64-bit floats.  A plan whose axes or pairs are not as make_plan writes them is refused.  inverse: by the negative angle, which is the gradient.
+ *     fp32: the product is formed in 64-bit floats.  inverse: by the negative angle, which is the gradient.  A plan with a pair on an axis that it
+ *     does not have is refused.
  */
 #define DROPIT_ROTARY_MAX_PAIRS 256
 #define DROPIT_ROTARY_MAX_AXES 8
@@ -382,7 +384,7 @@ dropit_status dropit_rotary(const dropit_rotary_plan* plan, int64_t batch, int64
  *   steps [device, int32 per ordinal]: steps taken; the call counts up those of its tensors (not those with n = 0).  ticket [device, one word]: zero
  *     before the first call, zero again after each; calls with the same ticket are ordered.  grad_factor [device] or NULL: multiplies the
  *     gradients (rounded to fp32, then squared).  lr_device [device] or NULL: read in the place of lr.
- * All tensors of a call have the same types; nothing is copied to the device, so that a captured call replays with its step number counting on.
+ * All tensors of a call have the same types, and fewer than 2^31 values each; nothing is copied to the device, so that a captured call replays with its step number counting on.
  */
 #define DROPIT_ADAMW_BLOCK 256
 typedef struct {
