@@ -182,7 +182,7 @@ __device__ __forceinline__ float approx_sqrt(float x) {
 }
 // The root to the nearest fp32 for x of 2^-102 and more: x times its approximate reciprocal root, and a Newton step whose residue is exact (P. Markstein,
 // "Computation of elementary functions on the IBM RISC System/6000 processor", 1990): compared with __fsqrt_rn for all of them.  Smaller ones, whose residue
-// has digits under 2^-149, take 2^64 first where ANY; so do zero, infinity and NaN, which are their own roots and come out as NaN without it.
+// has digits under 2^-149, are multiplied with 2^64 first where ANY.  Zero, infinity and NaN come out as NaN, with ANY as themselves.
 // 86.6 M values: 217 us; with __fsqrt_rn 5 more, with __frcp_rn too 9.
 constexpr float kSmallestFast = 0x1p-102f;
 template <bool ANY>

@@ -24,7 +24,7 @@ class DropITAdamW(torch.optim.Optimizer):
     master: bf16 parameters have an fp32 copy that is stepped in their place (state: master); fp32 ones need none.  The copy is made when the state is
         laid out: what is written to a parameter later is overwritten from it, and a parameter whose type has changed is refused.
     dither: bf16 parameters are rounded with a dither, which keeps small steps on average without a copy; else to nearest.
-    lr may be a CUDA tensor of one fp32 value, which a captured step reads when it replays.  step(grad_factor=t): gradients times t, a CUDA
+    lr may be a CUDA tensor of one fp32 value, which a captured step reads when it replays; other hyperparameters are part of the graph.  step(grad_factor=t): gradients times t, a CUDA
     tensor of one fp32 value (clipping, unscaling).  Parameters without a gradient stay as they are.  An infinite or NaN gradient
     spoils its own value, and in 8 bits the moments of its block of 256.
 
