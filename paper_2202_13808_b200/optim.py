@@ -103,6 +103,8 @@ class DropITAdamW(torch.optim.Optimizer):
         device = params[0].device
         if any(p.device != device for p in params) or device.type != "cuda":
             raise ValueError("all parameters must be on one CUDA device (there is no CPU path)")
+        if self._captured:
+            raise RuntimeError("a captured step holds the places of the state, which cannot be laid out again")
         if torch.cuda.is_current_stream_capturing():        # the zeros and copies below would be part of the graph, and every replay begin anew
             raise RuntimeError("the state must be laid out before a step is captured: call init_state()")
         spans = sorted((p.data_ptr(), p.data_ptr() + p.numel() * p.element_size()) for p in params if p.numel())
@@ -140,7 +142,7 @@ class DropITAdamW(torch.optim.Optimizer):
 
     def init_state(self, p=None):
         """Lay out the state now; returns state[p].  The first step does it otherwise, and the first one after add_param_group, but not under capture."""
-        if self._plan is None:
+        if self._plan is None or not self.state:
             self._build()
         return None if p is None else self.state[p]
 
@@ -218,7 +220,7 @@ class DropITAdamW(torch.optim.Optimizer):
         if closure is not None:
             with torch.enable_grad():
                 loss = closure()
-        if self._plan is None:
+        if self._plan is None or not self.state:        # emptied by the caller: begins anew
             self._build()
         settings = []
         for g in self.param_groups:

@@ -248,3 +248,29 @@ def test_hooks_around_a_checkpoint_see_its_state(cuda_device):
     opt.register_load_state_dict_post_hook(lambda o: seen.append(int(o.state[model.weight]["step"])))
     opt.load_state_dict(saved)
     assert seen == [[0, 1], 5]
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_a_state_that_is_emptied_begins_anew(cuda_device, bits):
+    model, other = _model(cuda_device), _model(cuda_device)
+    opt = dropit.DropITAdamW(model.parameters(), lr=1e-2, state_bits=bits)
+    _fill_grads(model, 1)
+    opt.step()
+    with torch.no_grad():
+        for p, q in zip(model.parameters(), other.parameters()):
+            q.copy_(p)
+    opt.state.clear()
+    _fill_grads(model, 2)
+    _fill_grads(other, 2)
+    opt.step()
+    fresh = dropit.DropITAdamW(other.parameters(), lr=1e-2, state_bits=bits)
+    fresh.step()
+    assert all(torch.equal(p, q) for p, q in zip(model.parameters(), other.parameters()))
+    assert _equal(_values(opt, model.parameters()), _values(fresh, other.parameters())) and len(opt.state_dict()["state"]) == 2
+    opt.state.clear()
+    assert int(opt.init_state(model.weight)["step"]) == 0
+    with torch.cuda.graph(torch.cuda.CUDAGraph()):
+        opt.step()
+    opt.state.clear()
+    with pytest.raises(RuntimeError, match="captured"):
+        opt.step()
